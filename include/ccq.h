@@ -268,6 +268,152 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
                               size_t ws_bytes, void* stream);
 
 /*
+ * ---- The gated delta rule without the query contraction ----
+ *
+ *     S_t = alpha_t S_{t-1} (I - beta_t k_t k_t^T) + beta_t v_t k_t^T,   o_t = scale S_t q_t
+ *
+ * (ccq_gdn_fwd with lambda = 0, without its key statistics), with query/key heads
+ * that several value heads share: value head h reads q and k of head h / (HV / HK).
+ *   q, k [B,T,HK,dk], v, o [B,T,HV,dv] io_dtype; logalpha, beta [B,T,HV] fp32;
+ *   S0, ST [B,HV,dv,dk] fp32 or NULL (zero; not wanted).
+ * ST is as exact as fp32 arithmetic makes it whatever io_dtype is (bf16 operands
+ * of the state's products are taken as head and tail), so the state may be handed
+ * from segment to segment and to ccq_delta_step without a loss.  o and the
+ * gradients carry bf16 products where io_dtype is bf16.
+ * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
+ * cu_seqlens of B + 1 int32, s->T a bound on the lengths; rows behind cu[B] (and
+ * behind a sequence's first T) are not written.
+ * Supported: dv in {64,128,256,512}; dk in {64,128,256} (bf16 io) or {64,128} (fp32
+ * io); the training step with fp32 io: dk = 64; ccq_delta_step: dk in {64,128,256},
+ * both types.  B > 65535 packed is CCQ_ERR_UNSUPPORTED.
+ */
+typedef struct {
+  int32_t B, T;         /* sequences, tokens (or the bound on them); >= 0 */
+  int32_t HK, HV;       /* query/key heads, value heads: HV a multiple of HK */
+  int32_t dk, dv;
+  ccq_dtype io_dtype;
+  float scale;
+} ccq_delta_shape;
+
+/* Bytes of workspace of the forward (with_bwd = 0) or the training step; 0: unsupported. */
+size_t ccq_delta_workspace_size(const ccq_delta_shape* s, int with_bwd);
+ccq_status ccq_delta_fwd(const ccq_delta_shape* s, const void* q, const void* k, const void* v,
+                         const float* logalpha, const float* beta, const float* S0, void* o,
+                         float* ST, void* workspace, size_t ws_bytes, void* stream);
+ccq_status ccq_delta_fwd_varlen(const ccq_delta_shape* s, const int32_t* cu_seqlens, const void* q,
+                                const void* k, const void* v, const float* logalpha,
+                                const float* beta, const float* S0, void* o, float* ST,
+                                void* workspace, size_t ws_bytes, void* stream);
+/*
+ * Training step: the gradients of L = sum_t <dO_t, o_t>, and o (NULL: not wanted, as
+ * where the forward has been run and dO came from what follows it) and ST (NULL: not
+ * wanted).  No gradient flows to S0 or from ST.  dq, dk [B,T,HK,dk] (summed over
+ * the value heads that share them, in fp32 and in order), dv [B,T,HV,dv],
+ * dlogalpha, dbeta [B,T,HV], all io_dtype.  Outputs may not overlap inputs.
+ */
+ccq_status ccq_delta_fwd_bwd(const ccq_delta_shape* s, const void* q, const void* k, const void* v,
+                             const float* logalpha, const float* beta, const float* S0,
+                             const void* dO, void* o, float* ST, void* dq, void* dk, void* dv,
+                             void* dlogalpha, void* dbeta, void* workspace, size_t ws_bytes,
+                             void* stream);
+ccq_status ccq_delta_fwd_bwd_varlen(const ccq_delta_shape* s, const int32_t* cu_seqlens,
+                                    const void* q, const void* k, const void* v,
+                                    const float* logalpha, const float* beta, const float* S0,
+                                    const void* dO, void* o, float* ST, void* dq, void* dk,
+                                    void* dv, void* dlogalpha, void* dbeta, void* workspace,
+                                    size_t ws_bytes, void* stream);
+/* The recurrent form for one or a few tokens (s->T of them) per sequence, on the
+ * state S [B,HV,dv,dk] fp32, updated in place; fp32 arithmetic; no workspace. */
+ccq_status ccq_delta_step(const ccq_delta_shape* s, const void* q, const void* k, const void* v,
+                          const float* logalpha, const float* beta, float* S, void* o,
+                          void* stream);
+
+/* Activations of the two operators below. */
+typedef enum { CCQ_ACT_NONE = 0, CCQ_ACT_SILU = 1, CCQ_ACT_SIGMOID = 2 } ccq_act;
+
+/*
+ * ---- Short causal convolution (what q, k and v pass before the recurrence) ----
+ *
+ *     y_t = act(bias + sum_{j<W} w_j x_{t-W+1+j})       every channel on its own
+ *
+ *   x [B,T,C] io_dtype, token pitch ldx elements (so a slice of a wider projection
+ *   can be read where it lies); w [C,W] fp32; bias [C] fp32 or NULL; y [B,T,C]
+ *   io_dtype, dense.  state0 [B,W-1,C] io_dtype: the W - 1 inputs before the first
+ *   token, oldest first (NULL: zeros); stateT the same after the last one (NULL: not
+ *   wanted; may not overlap state0).
+ * Supported: W in {2,3,4}, C a positive multiple of 8, ldx >= C with ldx elements a
+ * multiple of 16 bytes.  Packed batches: x, y [rows,C], offsets and T as above.
+ */
+typedef struct {
+  int32_t B, T, C, W;
+  ccq_dtype io_dtype;
+  ccq_act act;
+  int64_t ldx;
+} ccq_conv_shape;
+
+ccq_status ccq_conv_fwd(const ccq_conv_shape* s, const void* x, const float* w, const float* bias,
+                        const void* state0, void* y, void* stateT, void* stream);
+ccq_status ccq_conv_fwd_varlen(const ccq_conv_shape* s, const int32_t* cu_seqlens, const void* x,
+                               const float* w, const float* bias, const void* state0, void* y,
+                               void* stateT, void* stream);
+/* Gradients: dy [B,T,C] io_dtype, dense; dstateT [B,W-1,C] io_dtype or NULL (zeros), the
+ * gradient of stateT; dx [B,T,C] io_dtype, dense; dw [C,W], dbias [C] fp32 (dbias with
+ * bias only, else NULL); dstate0 [B,W-1,C] io_dtype or NULL (not wanted).  Outputs may
+ * not overlap inputs.  workspace: ccq_conv_workspace_size(s) bytes (0: unsupported). */
+size_t ccq_conv_workspace_size(const ccq_conv_shape* s);
+ccq_status ccq_conv_bwd(const ccq_conv_shape* s, const void* x, const float* w, const float* bias,
+                        const void* state0, const void* dy, const void* dstateT, void* dx,
+                        float* dw, float* dbias, void* dstate0, void* workspace, size_t ws_bytes,
+                        void* stream);
+ccq_status ccq_conv_bwd_varlen(const ccq_conv_shape* s, const int32_t* cu_seqlens, const void* x,
+                               const float* w, const float* bias, const void* state0,
+                               const void* dy, const void* dstateT, void* dx, float* dw,
+                               float* dbias, void* dstate0, void* workspace, size_t ws_bytes,
+                               void* stream);
+/* One token per sequence (s->T must be 1): x, y [B,C] (x with pitch ldx); state
+ * [B,W-1,C] io_dtype, moved on by the token in place. */
+ccq_status ccq_conv_step(const ccq_conv_shape* s, const void* x, const float* w, const float* bias,
+                         void* state, void* y, void* stream);
+
+/*
+ * ---- Group norm of the heads with an activation, channels last ----
+ *
+ * x is [rows, G, D] (a token's G heads of D channels): every head of every token is
+ * normalised on its own,
+ *   CCQ_NORM_GROUP  n = (x - mean x) / sqrt(var x + eps)
+ *   CCQ_NORM_RMS    n = x / sqrt(mean x^2 + eps)
+ *   CCQ_NORM_L2     n = x / sqrt(sum x^2 + eps)
+ * then z = n w + bias and y = z act(gate) with a gate, y = act(z) without.
+ *   x, gate [rows,G,D] io_dtype with row pitches ldx, ldg elements (a row's G D elements
+ *   are dense); w, bias [G,D] fp32, or [D] with shared = 1 (all heads take the same),
+ *   or NULL (ones, zeros; bias only with w); gate may be NULL; y [rows,G,D] io_dtype.
+ * Supported: D a multiple of 8 up to 8192, G D <= 2^24; ldx, ldg >= G D and a multiple of 16
+ * bytes (ldg is read with a gate only); eps >= 0.
+ */
+typedef enum { CCQ_NORM_GROUP = 0, CCQ_NORM_RMS = 1, CCQ_NORM_L2 = 2 } ccq_norm_kind;
+typedef struct {
+  int64_t rows;
+  int32_t G, D;
+  ccq_dtype io_dtype;
+  ccq_norm_kind kind;
+  ccq_act act;
+  int32_t shared;
+  float eps;
+  int64_t ldx, ldg;
+} ccq_norm_shape;
+
+ccq_status ccq_norm_fwd(const ccq_norm_shape* s, const void* x, const float* w, const float* bias,
+                        const void* gate, void* y, void* stream);
+/* Gradients: dy [rows,G,D] io_dtype, dense; dx, dgate [rows,G,D] io_dtype, dense (dgate with
+ * a gate only); dw, dbias fp32, shaped as w and bias (with them only; a shared weight's
+ * gradient is summed over the heads).  Outputs may not overlap inputs.  workspace:
+ * ccq_norm_workspace_size(s) bytes (0: unsupported), needed with w only. */
+size_t ccq_norm_workspace_size(const ccq_norm_shape* s);
+ccq_status ccq_norm_bwd(const ccq_norm_shape* s, const void* x, const float* w, const float* bias,
+                        const void* gate, const void* dy, void* dx, float* dw, float* dbias,
+                        void* dgate, void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Per-kernel timing hook (instrumentation for benchmarks and profilers, not
  * part of the method).  `events` points at n_events hipEvent_t handles created
  * by the caller (hipEventCreate).  Until the next ccq_trace_events call from

@@ -20,12 +20,18 @@ LIB_PATH = os.path.join(_PKG, "libccq.so")
 
 CCQ_F32, CCQ_BF16 = 0, 1
 CCQ_GLA, CCQ_GDN = 0, 1
+CCQ_ACT_NONE, CCQ_ACT_SILU, CCQ_ACT_SIGMOID = 0, 1, 2
+CCQ_NORM_GROUP, CCQ_NORM_RMS, CCQ_NORM_L2 = 0, 1, 2
 _STATUS = {0: "CCQ_OK", 1: "CCQ_ERR_INVALID_ARG", 2: "CCQ_ERR_UNSUPPORTED",
            3: "CCQ_ERR_WORKSPACE", 4: "CCQ_ERR_HIP"}
 EXPORTS = ("ccq_workspace_size", "ccq_gla_fwd", "ccq_gdn_fwd", "ccq_gdn_fwd_noalloc", "ccq_fwd_bwd",
            "ccq_varlen_workspace_size", "ccq_gla_fwd_varlen", "ccq_gdn_fwd_varlen",
            "ccq_fwd_bwd_varlen", "ccq_decode_workspace_size", "ccq_decode", "ccq_prep",
            "ccq_fwd_raw_workspace_size", "ccq_fwd_raw",
+           "ccq_delta_workspace_size", "ccq_delta_fwd", "ccq_delta_fwd_varlen", "ccq_delta_fwd_bwd",
+           "ccq_delta_fwd_bwd_varlen", "ccq_delta_step", "ccq_conv_workspace_size", "ccq_conv_fwd",
+           "ccq_conv_fwd_varlen", "ccq_conv_bwd", "ccq_conv_bwd_varlen", "ccq_conv_step",
+           "ccq_norm_workspace_size", "ccq_norm_fwd", "ccq_norm_bwd",
            "ccq_trace_events", "ccq_status_string", "ccq_version")
 
 
@@ -43,6 +49,28 @@ class Shape(ctypes.Structure):
                 ("io_dtype", ctypes.c_int32), ("gate_dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("centered", ctypes.c_int32),
                 ("decay_aligned", ctypes.c_int32), ("t0", ctypes.c_int64)]
+
+
+class DeltaShape(ctypes.Structure):
+    """Mirror of ccq_delta_shape."""
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("HK", ctypes.c_int32),
+                ("HV", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class ConvShape(ctypes.Structure):
+    """Mirror of ccq_conv_shape."""
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("C", ctypes.c_int32),
+                ("W", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("ldx", ctypes.c_int64)]
+
+
+class NormShape(ctypes.Structure):
+    """Mirror of ccq_norm_shape."""
+    _fields_ = [("rows", ctypes.c_int64), ("G", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("kind", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("shared", ctypes.c_int32), ("eps", ctypes.c_float), ("ldx", ctypes.c_int64),
+                ("ldg", ctypes.c_int64)]
 
 
 _lib = None
@@ -90,6 +118,25 @@ def lib() -> ctypes.CDLL:
             L.ccq_fwd_raw_workspace_size.restype = S
             L.ccq_fwd_raw.argtypes = [SP, ctypes.c_int] + [P] * 15 + [P, S, P]
             L.ccq_fwd_raw.restype = ctypes.c_int
+            for name, cls, n in (("ccq_delta_fwd", DeltaShape, 8), ("ccq_delta_fwd_varlen", DeltaShape, 9),
+                                 ("ccq_delta_fwd_bwd", DeltaShape, 14),
+                                 ("ccq_delta_fwd_bwd_varlen", DeltaShape, 15),
+                                 ("ccq_delta_step", DeltaShape, 7), ("ccq_conv_fwd", ConvShape, 6),
+                                 ("ccq_conv_fwd_varlen", ConvShape, 7),
+                                 ("ccq_conv_bwd", ConvShape, 10),
+                                 ("ccq_conv_bwd_varlen", ConvShape, 11),
+                                 ("ccq_conv_step", ConvShape, 5), ("ccq_norm_fwd", NormShape, 5),
+                                 ("ccq_norm_bwd", NormShape, 9)):
+                f = getattr(L, name)  # shape, tensors, [workspace, its size,] stream
+                work = "delta_fwd" in name or name.endswith("bwd") or "bwd_" in name
+                f.argtypes = [ctypes.POINTER(cls)] + [P] * n + ([P, S] if work else []) + [P]
+                f.restype = ctypes.c_int
+            L.ccq_delta_workspace_size.argtypes = [ctypes.POINTER(DeltaShape), ctypes.c_int]
+            L.ccq_delta_workspace_size.restype = S
+            L.ccq_conv_workspace_size.argtypes = [ctypes.POINTER(ConvShape)]
+            L.ccq_conv_workspace_size.restype = S
+            L.ccq_norm_workspace_size.argtypes = [ctypes.POINTER(NormShape)]
+            L.ccq_norm_workspace_size.restype = S
             L.ccq_trace_events.argtypes = [P, ctypes.c_int]
             L.ccq_trace_events.restype = ctypes.c_int
             L.ccq_status_string.argtypes = [ctypes.c_int]
@@ -624,3 +671,425 @@ def ccq_fwd_raw(q_raw, k_raw, w_lam, b_lam, v, gate, beta=None, backbone=CCQ_GLA
     if rc != 0:
         raise CcqError("ccq_fwd_raw", rc)
     return out
+
+
+# ---- The operators around the contraction: the plain gated delta rule, the short
+# convolution and the head norm.  Tensors given in `out` are checked like inputs and may
+# share no memory with the inputs or each other; a call is made on the tensors' own device.
+
+def _on_gpu(t, name):
+    if not t.is_cuda:
+        raise ValueError("%s: on %s, expected a GPU tensor" % (name, t.device))
+
+
+def _outputs(out, want, dev, inputs):
+    """The outputs named in `want` (name -> (shape, dtype)), from `out` where given."""
+    if not out:
+        return {n: torch.empty(shp, dtype=dt, device=dev) for n, (shp, dt) in want.items()}
+    extra = set(out) - set(want)
+    if extra:
+        raise ValueError("out: no output named %s here" % ", ".join(sorted(extra)))
+    spans = [_span(t) for t in inputs if t is not None]
+    res = {}
+    for n, (shp, dt) in want.items():
+        t = out.get(n)
+        if t is None:
+            t = torch.empty(shp, dtype=dt, device=dev)
+        else:
+            _check(t, n, shp, dt, dev)
+            a, b = _span(t)
+            if any(a < e and s < b for s, e in spans):
+                raise ValueError("%s: shares memory with an input or another output" % n)
+            spans.append((a, b))
+        res[n] = t
+    return res
+
+
+def _span(t):
+    """First and one past the last byte that a (possibly strided) tensor covers."""
+    if t.numel() == 0:
+        return 0, 0
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _pitch(t, inner, name):
+    """Row pitch of a tensor whose last `inner` dims are dense and whose leading dims step
+    evenly: a dense tensor, or a slice of a wider one."""
+    size = 1
+    for n in t.shape[t.dim() - inner:]:
+        size *= n
+    if t.is_contiguous():
+        return size
+    want = 1
+    for n, s in zip(reversed(t.shape[t.dim() - inner:]), reversed(t.stride()[t.dim() - inner:])):
+        if n != 1 and s != want:
+            raise ValueError("%s: the channels must be contiguous" % name)
+        want *= n
+    ld, rows = None, 1
+    for n, s in zip(reversed(t.shape[:t.dim() - inner]), reversed(t.stride()[:t.dim() - inner])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld = s
+        elif s != ld * rows:
+            raise ValueError("%s: its tokens must be evenly spaced" % name)
+        rows *= n
+    if ld is None:
+        return size
+    if ld < size:
+        raise ValueError("%s: its tokens overlap" % name)
+    return ld
+
+
+def _launch(name, dev, stream, shape, args, ws=None):
+    """Calls the library's function `name` with the tensors' device current."""
+    if stream is None:
+        handle = torch.cuda.current_stream(dev).cuda_stream
+    else:
+        if stream.device != dev:
+            raise ValueError("stream: on %s, the tensors on %s" % (stream.device, dev))
+        handle = stream.cuda_stream
+    ptrs = [None if t is None else t.data_ptr() for t in args]
+    if ws is not None:
+        ptrs += [ws.data_ptr(), ws.numel()] if isinstance(ws, torch.Tensor) else [None, 0]
+    fn = getattr(lib(), name)
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(shape, *ptrs, handle)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(shape, *ptrs, handle)
+    if rc != 0:
+        raise CcqError(name, rc)
+
+
+def _scratch(workspace, need, dev):
+    """The caller's workspace or a new one; () where none is needed."""
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=dev) if need else ()
+    if workspace.device != dev or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous uint8 tensor on %s is expected" % dev)
+    return workspace
+
+
+def _check_offsets(cu_seqlens, dev):
+    if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+        raise TypeError("cu_seqlens must be a 1-D int32 tensor of B + 1 offsets")
+    if cu_seqlens.device != dev or not cu_seqlens.is_contiguous():
+        raise ValueError("cu_seqlens must be contiguous on the tensors' device")
+
+
+def make_delta_shape(B, T, HK, HV, dk, dv, io_dtype, scale=1.0) -> DeltaShape:
+    return DeltaShape(int(B), int(T), int(HK), int(HV), int(dk), int(dv), _dt(io_dtype),
+                      float(scale))
+
+
+def ccq_delta_workspace_size(shape: DeltaShape, with_bwd: bool = False) -> int:
+    return int(lib().ccq_delta_workspace_size(ctypes.byref(shape), int(bool(with_bwd))))
+
+
+def _delta_shape(q, k, v, logalpha, beta, cu_seqlens, max_len, scale):
+    """Checks the inputs of the chunked forms; returns the shape and the token dims."""
+    dims = 4 if cu_seqlens is None else 3
+    _on_gpu(q, "q")
+    if q.dim() != dims or v.dim() != dims:
+        raise ValueError("q and v: %d dims expected" % dims)
+    dev, dt = q.device, q.dtype
+    HK, dk = q.shape[-2:]
+    HV, dv = v.shape[-2:]
+    tok = tuple(q.shape[:-2])
+    if cu_seqlens is None:
+        B, T = tok
+    else:
+        _check_offsets(cu_seqlens, dev)
+        B, T = cu_seqlens.numel() - 1, max_len
+    shape = make_delta_shape(B, T, HK, HV, dk, dv, dt, scale)
+    _check(q, "q", q.shape, dt, dev)
+    _check(k, "k", q.shape, dt, dev)
+    _check(v, "v", tok + (HV, dv), dt, dev)
+    _check(logalpha, "logalpha", tok + (HV,), torch.float32, dev)
+    _check(beta, "beta", tok + (HV,), torch.float32, dev)
+    return shape, tok
+
+
+def _delta_fwd(q, k, v, logalpha, beta, cu_seqlens, max_len, S0, scale, want_states, out,
+               workspace, stream):
+    shape, tok = _delta_shape(q, k, v, logalpha, beta, cu_seqlens, max_len, scale)
+    dev = q.device
+    state = (shape.B, shape.HV, shape.dv, shape.dk)
+    _check(S0, "S0", state, torch.float32, dev)
+    want = {"o": (tuple(v.shape), q.dtype)}
+    if want_states:
+        want["ST"] = (state, torch.float32)
+    res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0))
+    ws = _scratch(workspace, ccq_delta_workspace_size(shape), dev)
+    args = [q, k, v, logalpha, beta, S0, res["o"], res.get("ST")]
+    if cu_seqlens is None:
+        _launch("ccq_delta_fwd", dev, stream, shape, args, ws)
+    else:
+        _launch("ccq_delta_fwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
+    _record(stream, ws, res)
+    return res
+
+
+def ccq_delta_fwd(q, k, v, logalpha, beta, S0=None, scale=1.0, want_states=True, out=None,
+                  workspace=None, stream=None):
+    """The gated delta rule without the contraction: q, k [B,T,HK,dk], v [B,T,HV,dv] (value
+    head h reads q and k of head h // (HV // HK)), logalpha, beta [B,T,HV] fp32, S0
+    [B,HV,dv,dk] fp32.  Returns dict o [B,T,HV,dv][, ST]."""
+    return _delta_fwd(q, k, v, logalpha, beta, None, None, S0, scale, want_states, out, workspace,
+                      stream)
+
+
+def ccq_delta_fwd_varlen(q, k, v, logalpha, beta, cu_seqlens, max_len, S0=None, scale=1.0,
+                         want_states=True, out=None, workspace=None, stream=None):
+    """ccq_delta_fwd on a packed batch: q, k [rows,HK,dk], v [rows,HV,dv], logalpha, beta
+    [rows,HV]; sequence b is rows cu_seqlens[b]..cu_seqlens[b+1]-1, at most max_len long."""
+    return _delta_fwd(q, k, v, logalpha, beta, cu_seqlens, max_len, S0, scale, want_states, out,
+                      workspace, stream)
+
+
+def _delta_fwd_bwd(q, k, v, logalpha, beta, dO, cu_seqlens, max_len, S0, scale, want_o,
+                   want_states, out, workspace, stream):
+    shape, tok = _delta_shape(q, k, v, logalpha, beta, cu_seqlens, max_len, scale)
+    dev, dt = q.device, q.dtype
+    state = (shape.B, shape.HV, shape.dv, shape.dk)
+    _check(S0, "S0", state, torch.float32, dev)
+    _check(dO, "dO", v.shape, dt, dev)
+    gates = tok + (shape.HV,)
+    want = {"dq": (tuple(q.shape), dt), "dk": (tuple(q.shape), dt), "dv": (tuple(v.shape), dt),
+            "dlogalpha": (gates, dt), "dbeta": (gates, dt)}
+    if want_o:
+        want["o"] = (tuple(v.shape), dt)
+    if want_states:
+        want["ST"] = (state, torch.float32)
+    res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0, dO))
+    ws = _scratch(workspace, ccq_delta_workspace_size(shape, True), dev)
+    args = [q, k, v, logalpha, beta, S0, dO, res.get("o"), res.get("ST"), res["dq"], res["dk"],
+            res["dv"], res["dlogalpha"], res["dbeta"]]
+    if cu_seqlens is None:
+        _launch("ccq_delta_fwd_bwd", dev, stream, shape, args, ws)
+    else:
+        _launch("ccq_delta_fwd_bwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
+    _record(stream, ws, res)
+    return res
+
+
+def ccq_delta_fwd_bwd(q, k, v, logalpha, beta, dO, S0=None, scale=1.0, want_o=True,
+                      want_states=False, out=None, workspace=None, stream=None):
+    """Training step of ccq_delta_fwd: the gradients of sum <dO, o>, in q's dtype.  Returns dict
+    dq, dk (summed over the value heads that share them), dv, dlogalpha, dbeta[, o][, ST];
+    want_o=False where the forward has been run already.  No gradient flows to S0."""
+    return _delta_fwd_bwd(q, k, v, logalpha, beta, dO, None, None, S0, scale, want_o, want_states,
+                          out, workspace, stream)
+
+
+def ccq_delta_fwd_bwd_varlen(q, k, v, logalpha, beta, dO, cu_seqlens, max_len, S0=None, scale=1.0,
+                             want_o=True, want_states=False, out=None, workspace=None,
+                             stream=None):
+    """ccq_delta_fwd_bwd on a packed batch (layout as ccq_delta_fwd_varlen)."""
+    return _delta_fwd_bwd(q, k, v, logalpha, beta, dO, cu_seqlens, max_len, S0, scale, want_o,
+                          want_states, out, workspace, stream)
+
+
+def ccq_delta_step(q, k, v, logalpha, beta, S, scale=1.0, out=None, stream=None):
+    """The recurrent form for one or a few tokens: q, k [B,T,HK,dk], v [B,T,HV,dv], logalpha,
+    beta [B,T,HV] fp32; the state S [B,HV,dv,dk] fp32 is updated in place.  Returns o."""
+    _on_gpu(q, "q")
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v: 4 dims expected")
+    if S is None:
+        raise ValueError("S (the state) is required")
+    B, T, HK, dk = q.shape
+    HV, dv = v.shape[2:]
+    dev, dt, f32 = q.device, q.dtype, torch.float32
+    for t, name, shp, d in ((q, "q", q.shape, dt), (k, "k", q.shape, dt),
+                            (v, "v", (B, T, HV, dv), dt), (logalpha, "logalpha", (B, T, HV), f32),
+                            (beta, "beta", (B, T, HV), f32), (S, "S", (B, HV, dv, dk), f32)):
+        _check(t, name, shp, d, dev)
+    if out is None:
+        o = torch.empty((B, T, HV, dv), dtype=dt, device=dev)
+    else:
+        o = _outputs({"o": out}, {"o": ((B, T, HV, dv), dt)}, dev,
+                     (q, k, v, logalpha, beta, S))["o"]
+    shape = DeltaShape(B, T, HK, HV, dk, dv, _dt(dt), scale)
+    _launch("ccq_delta_step", dev, stream, shape, (q, k, v, logalpha, beta, S, o))
+    if stream is not None:
+        _record(stream, o)
+    return o
+
+
+def _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act):
+    dims = 3 if cu_seqlens is None else 2
+    _on_gpu(x, "x")
+    if x.dim() != dims or w.dim() != 2:
+        raise ValueError("x: %d dims, w: 2 dims expected" % dims)
+    dev, dt = x.device, x.dtype
+    C, W = w.shape
+    if x.shape[-1] != C:
+        raise ValueError("x: %d channels, w has %d" % (x.shape[-1], C))
+    if cu_seqlens is None:
+        B, T = x.shape[:2]
+    else:
+        _check_offsets(cu_seqlens, dev)
+        B, T = cu_seqlens.numel() - 1, max_len
+    _check(w, "w", (C, W), torch.float32, dev)
+    _check(bias, "bias", (C,), torch.float32, dev)
+    _check(state0, "state0", (B, W - 1, C), dt, dev)
+    return ConvShape(B, int(T), C, W, _dt(dt), int(act), _pitch(x, 1, "x"))
+
+
+def _conv_fwd(x, w, cu_seqlens, max_len, bias, state0, act, want_state, out, stream):
+    shape = _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act)
+    dev = x.device
+    want = {"y": (tuple(x.shape), x.dtype)}
+    if want_state:
+        want["stateT"] = ((shape.B, shape.W - 1, shape.C), x.dtype)
+    res = _outputs(out, want, dev, (x, w, bias, state0))
+    args = [x, w, bias, state0, res["y"], res.get("stateT")]
+    if cu_seqlens is None:
+        _launch("ccq_conv_fwd", dev, stream, shape, args)
+    else:
+        _launch("ccq_conv_fwd_varlen", dev, stream, shape, [cu_seqlens] + args)
+    _record(stream, res)
+    return res
+
+
+def ccq_conv_fwd(x, w, bias=None, state0=None, act=CCQ_ACT_SILU, want_state=False, out=None,
+                 stream=None):
+    """Short causal convolution of every channel, y = act(bias + sum_j w[:, j] x_{t-W+1+j}):
+    x [B,T,C] (dense, or a slice of a wider tensor), w [C,W] fp32 (W = 2, 3, 4), bias [C] fp32,
+    state0 [B,W-1,C] the inputs before the first token, oldest first.  Returns dict y[, stateT]."""
+    return _conv_fwd(x, w, None, None, bias, state0, act, want_state, out, stream)
+
+
+def ccq_conv_fwd_varlen(x, w, cu_seqlens, max_len, bias=None, state0=None, act=CCQ_ACT_SILU,
+                        want_state=False, out=None, stream=None):
+    """ccq_conv_fwd on a packed batch: x [rows,C]; sequence b is rows
+    cu_seqlens[b]..cu_seqlens[b+1]-1, at most max_len long."""
+    return _conv_fwd(x, w, cu_seqlens, max_len, bias, state0, act, want_state, out, stream)
+
+
+def _conv_bwd(x, w, dy, cu_seqlens, max_len, bias, state0, dstateT, act, out, workspace, stream):
+    shape = _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act)
+    dev, dt, f32 = x.device, x.dtype, torch.float32
+    state = (shape.B, shape.W - 1, shape.C)
+    _check(dy, "dy", x.shape, dt, dev)
+    _check(dstateT, "dstateT", state, dt, dev)
+    want = {"dx": (tuple(x.shape), dt), "dw": (tuple(w.shape), f32)}
+    if bias is not None:
+        want["dbias"] = (tuple(bias.shape), f32)
+    if state0 is not None:
+        want["dstate0"] = (state, dt)
+    res = _outputs(out, want, dev, (x, w, bias, state0, dy, dstateT))
+    ws = _scratch(workspace, int(lib().ccq_conv_workspace_size(shape)), dev)
+    args = [x, w, bias, state0, dy, dstateT, res["dx"], res["dw"], res.get("dbias"),
+            res.get("dstate0")]
+    if cu_seqlens is None:
+        _launch("ccq_conv_bwd", dev, stream, shape, args, ws)
+    else:
+        _launch("ccq_conv_bwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
+    _record(stream, ws, res)
+    return res
+
+
+def ccq_conv_bwd(x, w, dy, bias=None, state0=None, dstateT=None, act=CCQ_ACT_SILU, out=None,
+                 workspace=None, stream=None):
+    """Gradients of ccq_conv_fwd for dy [B,T,C] (and dstateT, the gradient of stateT).  Returns
+    dict dx, dw[, dbias][, dstate0]."""
+    return _conv_bwd(x, w, dy, None, None, bias, state0, dstateT, act, out, workspace, stream)
+
+
+def ccq_conv_bwd_varlen(x, w, dy, cu_seqlens, max_len, bias=None, state0=None, dstateT=None,
+                        act=CCQ_ACT_SILU, out=None, workspace=None, stream=None):
+    """ccq_conv_bwd on a packed batch (layout as ccq_conv_fwd_varlen)."""
+    return _conv_bwd(x, w, dy, cu_seqlens, max_len, bias, state0, dstateT, act, out, workspace,
+                     stream)
+
+
+def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=None):
+    """One token per sequence: x [B,C]; state [B,W-1,C] is moved on by the token in place.
+    Returns y [B,C]."""
+    _on_gpu(x, "x")
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w: 2 dims expected")
+    if state is None:
+        raise ValueError("state is required")
+    B, C = x.shape
+    W = w.shape[1]
+    dev, dt = x.device, x.dtype
+    _check(w, "w", (C, W), torch.float32, dev)
+    _check(bias, "bias", (C,), torch.float32, dev)
+    _check(state, "state", (B, W - 1, C), dt, dev)
+    if out is None:
+        y = torch.empty((B, C), dtype=dt, device=dev)
+    else:
+        y = _outputs({"y": out}, {"y": ((B, C), dt)}, dev, (x, w, bias, state))["y"]
+    shape = ConvShape(B, 1, C, W, _dt(dt), int(act), _pitch(x, 1, "x"))
+    _launch("ccq_conv_step", dev, stream, shape, (x, w, bias, state, y))
+    if stream is not None:
+        _record(stream, y)
+    return y
+
+
+def _norm_shape(x, weight, bias, gate, kind, act, eps):
+    _on_gpu(x, "x")
+    if x.dim() < 2:
+        raise ValueError("x: [..., G, D] expected")
+    G, D = x.shape[-2:]
+    rows = 1
+    for n in x.shape[:-2]:
+        rows *= n
+    dev, dt = x.device, x.dtype
+    shared = weight is not None and weight.dim() == 1
+    wshape = (D,) if shared else (G, D)
+    _check(weight, "weight", wshape, torch.float32, dev)
+    _check(bias, "bias", wshape, torch.float32, dev)
+    ldg = G * D
+    if gate is not None:
+        if gate.shape != x.shape or gate.dtype != dt or gate.device != dev:
+            _check(gate, "gate", x.shape, dt, dev)
+        ldg = _pitch(gate, 2, "gate")
+    return NormShape(rows, G, D, _dt(dt), int(kind), int(act), int(shared), float(eps),
+                     _pitch(x, 2, "x"), ldg)
+
+
+def ccq_norm_fwd(x, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, act=CCQ_ACT_SILU,
+                 eps=1e-5, out=None, stream=None):
+    """Group norm of every token's heads, channels last: x [..., G, D] (dense, or a slice of a
+    wider tensor), each head of each token normalised on its own (kind: CCQ_NORM_GROUP, _RMS,
+    _L2), z = n weight + bias with weight, bias [G,D] or, for all heads alike, [D] fp32;
+    returns z act(gate) with a gate [..., G, D], else act(z)."""
+    shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
+    dev = x.device
+    if out is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    else:
+        y = _outputs({"y": out}, {"y": (tuple(x.shape), x.dtype)}, dev, (x, weight, bias, gate))["y"]
+    _launch("ccq_norm_fwd", dev, stream, shape, (x, weight, bias, gate, y))
+    if stream is not None:
+        _record(stream, y)
+    return y
+
+
+def ccq_norm_bwd(x, dy, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, act=CCQ_ACT_SILU,
+                 eps=1e-5, out=None, workspace=None, stream=None):
+    """Gradients of ccq_norm_fwd for dy [..., G, D].  Returns dict dx[, dweight][, dbias][, dgate]."""
+    shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
+    dev, dt, f32 = x.device, x.dtype, torch.float32
+    _check(dy, "dy", x.shape, dt, dev)
+    want = {"dx": (tuple(x.shape), dt)}
+    if weight is not None:
+        want["dweight"] = (tuple(weight.shape), f32)
+    if bias is not None:
+        want["dbias"] = (tuple(bias.shape), f32)
+    if gate is not None:
+        want["dgate"] = (tuple(x.shape), dt)
+    res = _outputs(out, want, dev, (x, dy, weight, bias, gate))
+    need = int(lib().ccq_norm_workspace_size(shape)) if weight is not None else 0
+    ws = _scratch(workspace, need, dev)
+    _launch("ccq_norm_bwd", dev, stream, shape,
+            (x, weight, bias, gate, dy, res["dx"], res.get("dweight"), res.get("dbias"),
+             res.get("dgate")), ws)
+    _record(stream, ws, res)
+    return res

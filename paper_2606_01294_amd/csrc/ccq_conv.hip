@@ -1,0 +1,381 @@
+// ccq_conv.hip -- short causal convolution of every channel on its own, with an
+// activation: forward, backward and the one-token step.
+//
+//   z_t = b + sum_{j<W} w_j x_{t-W+1+j},   y_t = act(z_t),
+// where x at the W - 1 positions before a sequence's first token is its initial
+// state (or zero).  Backward, with dz = dy act'(z) (z formed again) and dz = 0
+// behind the last token:
+//   dx_p = sum_{i<W} w_{W-1-i} dz_{p+i}     (p < 0: the initial state's gradient),
+//   dw_j = sum_t dz_t x_{t-W+1+j},   db = sum_t dz_t.
+//
+// HBM bounds all three: x (and dy) are read and y (dx) written once.  A lane owns
+// a vector of channels and walks a run of consecutive tokens with the window of
+// the last W inputs in registers, so a row is read again only by the next run's
+// W - 1 tokens of overlap (from cache).  The rows of a batch are requested
+// together.  The backward's dw and db are summed in registers over a run, over the
+// four runs of a workgroup through LDS, and over the workgroups by a second kernel
+// in a fixed order.
+// Products and sums are fp32; y and dx are rounded once.
+#include "ccq_device.h"
+#include "ccq_kernels.h"
+#include "ccq_pointwise.h"
+
+namespace ccq {
+
+namespace {
+constexpr int kConvThreads = 256;
+constexpr int kConvRun = 32;   // tokens per lane, forward
+constexpr int kConvRunB = 32;  // backward
+
+// The taps of VE channels: w[c][j], consecutive in memory, 16-byte loads.
+template <int W, int VE>
+__device__ __forceinline__ void load_taps(float (&w)[W][VE], const float* p) {
+  float flat[W * VE];
+#pragma unroll
+  for (int i = 0; i < W * VE / 4; ++i) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + 4 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) flat[4 * i + e] = v[e];
+  }
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) w[j][e] = flat[e * W + j];
+}
+template <int VE>
+__device__ __forceinline__ void load_bias(float (&b)[VE], const float* p, int c) {
+#pragma unroll
+  for (int e = 0; e < VE; ++e) b[e] = p ? p[c + e] : 0.f;
+}
+}  // namespace
+
+template <typename T, int W, int VE>
+__global__ __launch_bounds__(kConvThreads) void conv_fwd_kernel(const ConvArgs a) {
+  typedef VecN<T, VE> V;
+  constexpr int NB = 8;  // rows requested together
+  const int CV = a.C / VE;
+  const unsigned id = blockIdx.x * kConvThreads + threadIdx.x;
+  const unsigned rr = id / CV;  // run, over all sequences
+  if (rr >= (unsigned)(a.B * a.runs)) return;
+  const int c = (int)(id - rr * CV) * VE;
+  const int b = rr / a.runs, run = rr - b * a.runs;
+  const Seq sq = seq_of(a.cu, b, a.T);
+  const int t0 = run * kConvRun;
+  if (run > 0 && t0 >= sq.len) return;
+  const int t1 = min(t0 + kConvRun, sq.len);
+  const T* x = static_cast<const T*>(a.x) + (size_t)sq.row0 * a.ldx + c;
+  const T* s0 = static_cast<const T*>(a.state0) + (size_t)b * (W - 1) * a.C + c;
+  T* y = static_cast<T*>(a.y) + (size_t)sq.row0 * a.C + c;
+  float w[W][VE], bias[VE], win[W][VE];
+  load_taps<W, VE>(w, a.w + (size_t)c * W);
+  load_bias<VE>(bias, a.bias, c);
+  // row p of the sequence, from the initial state where p < 0
+  auto row = [&](int p, float (&v)[VE]) {
+    if (p >= 0) {
+      const auto r = V::load(x + (size_t)p * a.ldx);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = V::get(r, e);
+    } else if (a.state0) {
+      const auto r = V::load(s0 + (size_t)(p + W - 1) * a.C);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = V::get(r, e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = 0.f;
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) row(t0 - (W - 1) + j, win[j + 1]);
+
+  for (int tb = t0; tb < t1; tb += NB) {
+    typename V::raw r[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) r[i] = V::load(x + (size_t)min(tb + i, t1 - 1) * a.ldx);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) win[j][e] = win[j + 1][e];
+      float o[VE];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        win[W - 1][e] = V::get(r[i], e);
+        float z = bias[e];
+#pragma unroll
+        for (int j = 0; j < W; ++j) z += w[j][e] * win[j][e];
+        o[e] = Act<T>::value(a.act, z);
+      }
+      if (tb + i < t1) V::store(y + (size_t)(tb + i) * a.C, o);
+    }
+  }
+  // the last run (or the only one of an empty sequence) leaves the final state,
+  // the last W - 1 inputs
+  if (a.stateT && t1 == sq.len) {
+    T* sT = static_cast<T*>(a.stateT) + (size_t)b * (W - 1) * a.C + c;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      float v[VE];
+      row(sq.len - (W - 1) + j, v);
+      V::store(sT + (size_t)j * a.C, v);
+    }
+  }
+}
+
+// One token per sequence: x [B, C], the state [B, W - 1, C] moved on in place.
+template <typename T, int W, int VE>
+__global__ __launch_bounds__(kConvThreads) void conv_step_kernel(const ConvArgs a) {
+  typedef VecN<T, VE> V;
+  const int CV = a.C / VE;
+  const unsigned id = blockIdx.x * kConvThreads + threadIdx.x;
+  const unsigned b = id / CV;
+  if (b >= (unsigned)a.B) return;
+  const int c = (int)(id - b * CV) * VE;
+  T* st = static_cast<T*>(a.stateT) + (size_t)b * (W - 1) * a.C + c;
+  typename V::raw r[W];
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) r[j] = V::load(st + (size_t)j * a.C);
+  r[W - 1] = V::load(static_cast<const T*>(a.x) + (size_t)b * a.ldx + c);
+  float w[W][VE], o[VE];
+  load_taps<W, VE>(w, a.w + (size_t)c * W);
+  load_bias<VE>(o, a.bias, c);
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[e] += w[j][e] * V::get(r[j], e);
+    o[e] = Act<T>::value(a.act, o[e]);
+  }
+  V::store(static_cast<T*>(a.y) + (size_t)b * a.C + c, o);
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) *reinterpret_cast<typename V::raw*>(st + (size_t)j * a.C) = r[j + 1];
+}
+
+// Workgroup: 64 channel vectors x 4 consecutive runs (a wave each) of one
+// sequence.  Its sums go to partial row blockIdx.x / column blocks: W planes of
+// C columns for dw, one for db.
+template <typename T, int W, int VE>
+__global__ __launch_bounds__(kConvThreads) void conv_bwd_kernel(const ConvArgs a) {
+  typedef VecN<T, VE> V;
+  constexpr int NB = 4;
+  __shared__ float buf[4][W + 1][64 * VE];
+  const int CV = a.C / VE, ncb = (CV + 63) / 64;
+  const unsigned rb = blockIdx.x / ncb;  // partial row: sequence and group of four runs
+  const int cb = blockIdx.x - rb * ncb;
+  const int groups = (a.runs + 3) / 4;
+  const int b = rb / groups, run = 4 * (int)(rb - b * groups) + wave_id();
+  const int cv = cb * 64 + lane_id();
+  const bool mine = cv < CV;
+  const int c = mine ? cv * VE : 0;
+  const Seq sq = seq_of(a.cu, b, a.T);
+  const int t0 = run * kConvRunB;
+
+  float dw[W][VE], db[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    db[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j][e] = 0.f;
+  }
+  if (mine && (run == 0 || t0 < sq.len)) {
+    const int t1 = min(t0 + kConvRunB, sq.len);
+    const T* x = static_cast<const T*>(a.x) + (size_t)sq.row0 * a.ldx + c;
+    const T* dy = static_cast<const T*>(a.dy) + (size_t)sq.row0 * a.C + c;
+    T* dx = static_cast<T*>(a.dx) + (size_t)sq.row0 * a.C + c;
+    const T* s0 = static_cast<const T*>(a.state0) + (size_t)b * (W - 1) * a.C + c;
+    const T* dsT = static_cast<const T*>(a.dstateT) + (size_t)b * (W - 1) * a.C + c;
+    T* ds0 = static_cast<T*>(a.dstate0) + (size_t)b * (W - 1) * a.C + c;
+    float w[W][VE], bias[VE], win[W][VE], dz[W][VE];
+    load_taps<W, VE>(w, a.w + (size_t)c * W);
+    load_bias<VE>(bias, a.bias, c);
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        win[j][e] = 0.f;
+        dz[j][e] = 0.f;
+      }
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      const int p = t0 - (W - 1) + j;
+      if (p >= 0 || a.state0) {
+        const auto r = V::load(p >= 0 ? x + (size_t)p * a.ldx : s0 + (size_t)(p + W - 1) * a.C);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) win[j + 1][e] = V::get(r, e);
+      }
+    }
+    // tokens t0 .. t1 + W - 2: the last W - 1 only complete the dx before them
+    const int te = t1 + W - 1;
+    for (int tb = t0; tb < te; tb += NB) {
+      typename V::raw rx[NB], rd[NB];
+      if (tb < sq.len)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const int t = min(tb + i, sq.len - 1);
+          rx[i] = V::load(x + (size_t)t * a.ldx);
+          rd[i] = V::load(dy + (size_t)t * a.C);
+        }
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int t = tb + i;
+        if (t >= te) break;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            win[j][e] = win[j + 1][e];
+            dz[j][e] = dz[j + 1][e];
+          }
+        if (t < sq.len) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            win[W - 1][e] = V::get(rx[i], e);
+            float z = bias[e], v, d;
+#pragma unroll
+            for (int j = 0; j < W; ++j) z += w[j][e] * win[j][e];
+            Act<T>::both(a.act, z, v, d);
+            dz[W - 1][e] = V::get(rd[i], e) * d;
+          }
+          if (t < t1)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              db[e] += dz[W - 1][e];
+#pragma unroll
+              for (int j = 0; j < W; ++j) dw[j][e] += dz[W - 1][e] * win[j][e];
+            }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) dz[W - 1][e] = 0.f;
+        }
+        // dx of p = t - W + 1 is complete: dz[i] holds token p + i
+        const int p = t - (W - 1);
+        if (p >= t0 || (p < 0 && a.dstate0)) {
+          float o[VE];
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            o[e] = 0.f;
+#pragma unroll
+            for (int q = 0; q < W; ++q) o[e] += w[W - 1 - q][e] * dz[q][e];
+          }
+          const int k = p - (sq.len - (W - 1));  // its row of the final state
+          if (a.dstateT && k >= 0) {
+            const auto r = V::load(dsT + (size_t)k * a.C);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) o[e] += V::get(r, e);
+          }
+          V::store(p >= 0 ? dx + (size_t)p * a.C : ds0 + (size_t)(p + W - 1) * a.C, o);
+        }
+      }
+    }
+  }
+
+  if (!a.part) return;
+  const int l = lane_id(), wv = wave_id();
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) buf[wv][j][l * VE + e] = dw[j][e];
+    buf[wv][W][l * VE + e] = db[e];
+  }
+  __syncthreads();
+  const int cols = min(64 * VE, a.C - cb * 64 * VE);
+  for (int i = threadIdx.x; i < (W + 1) * 64 * VE; i += kConvThreads) {
+    const int j = i / (64 * VE), k = i % (64 * VE);
+    if (k < cols)
+      a.part[((size_t)rb * (W + 1) + j) * a.C + cb * 64 * VE + k] =
+          (buf[0][j][k] + buf[1][j][k]) + (buf[2][j][k] + buf[3][j][k]);
+  }
+}
+
+namespace {
+// 16-byte vectors; the backward holds twice as much per channel and takes four
+// channels a lane.
+template <typename T> constexpr int conv_ve() { return 16 / (int)sizeof(T); }
+constexpr int kConvVeB = 4;
+
+int conv_runs(int T, int len) { return T > 0 ? (T + len - 1) / len : 1; }
+
+template <typename T, int W>
+hipError_t run_conv(ConvArgs a, ConvCall call, hipStream_t st) {
+  if (call == ConvCall::kBwd) {
+    a.runs = conv_runs(a.T, kConvRunB);
+    const long long ncb = (a.C / kConvVeB + 63) / 64;
+    const long long nblk = conv_part_rows(a.B, a.T) * ncb;
+    hipLaunchKernelGGL((conv_bwd_kernel<T, W, kConvVeB>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
+    return hipGetLastError();
+  }
+  constexpr int VE = conv_ve<T>();
+  const long long cv = a.C / VE;
+  if (call == ConvCall::kStep) {
+    const long long nblk = (a.B * cv + kConvThreads - 1) / kConvThreads;
+    hipLaunchKernelGGL((conv_step_kernel<T, W, VE>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
+    return hipGetLastError();
+  }
+  a.runs = conv_runs(a.T, kConvRun);
+  const long long nblk = ((long long)a.B * a.runs * cv + kConvThreads - 1) / kConvThreads;
+  hipLaunchKernelGGL((conv_fwd_kernel<T, W, VE>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t conv_dispatch(const ConvArgs& a, int W, ConvCall call, hipStream_t st) {
+  switch (W) {
+    case 2: return run_conv<T, 2>(a, call, st);
+    case 3: return run_conv<T, 3>(a, call, st);
+    case 4: return run_conv<T, 4>(a, call, st);
+  }
+  return hipErrorInvalidValue;
+}
+}  // namespace
+
+// Thread indices are 32 bits wide.
+bool conv_supported(int B, int T, int C, int W) {
+  if (W < 2 || W > 4 || C < 8 || C % 8) return false;
+  const long long runs = conv_runs(T, kConvRun);
+  return (long long)B * runs * (C / 4) < (1ll << 31) - kConvThreads;
+}
+long long conv_part_rows(int B, int T) { return (long long)B * ((conv_runs(T, kConvRunB) + 3) / 4); }
+
+hipError_t launch_conv(const ConvArgs& a, int W, ConvCall call, bool is_bf16, hipStream_t st) {
+  return is_bf16 ? conv_dispatch<bf16_t>(a, W, call, st) : conv_dispatch<float>(a, W, call, st);
+}
+
+// ----------------------------------------------------------------------------
+// Column sums of a [rows, cols] matrix of partial sums, in a fixed order: 32
+// columns per workgroup, 32 threads sharing a column's rows.
+namespace {
+constexpr int kSumCols = 32, kSumRows = 32;
+}
+__global__ __launch_bounds__(kSumCols * kSumRows) void colsum_kernel(const ColsumArgs a) {
+  __shared__ float buf[kSumRows][kSumCols + 1];
+  const int cl = threadIdx.x % kSumCols, rl = threadIdx.x / kSumCols;
+  const int col = blockIdx.x * kSumCols + cl;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (col < a.cols) {
+    const float* p = a.part + col;
+    long long r = rl;
+    for (; r + 3 * kSumRows < a.rows; r += 4 * kSumRows)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s[q] += p[(size_t)(r + q * kSumRows) * a.cols];
+    for (; r < a.rows; r += kSumRows) s[0] += p[(size_t)r * a.cols];
+  }
+  buf[rl][cl] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (rl == 0 && col < a.cols) {
+    float t = 0.f;
+#pragma unroll
+    for (int q = 0; q < kSumRows; ++q) t += buf[q][cl];
+    if (col >= a.first) {
+      if (a.out1) a.out1[col - a.first] = t;
+    } else if (a.taps) {
+      a.out0[(size_t)(col % a.C) * a.taps + col / a.C] = t;  // plane j, channel c -> [c][j]
+    } else {
+      a.out0[col] = t;
+    }
+  }
+}
+
+hipError_t launch_colsum(const ColsumArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(colsum_kernel, dim3((a.cols + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumRows), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace ccq

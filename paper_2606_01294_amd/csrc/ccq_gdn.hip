@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   float* const sA = reinterpret_cast<float*>(sKAX);
   float* const sX = sA + C * LDA;
   __shared__ __align__(16) float sY[4][16 * 17];
-  __shared__ __align__(16) float sGam[C], sBeta[C];
+  __shared__ __align__(16) float sGam[C], sGamLo[C], sBeta[C];
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
@@ -66,12 +66,15 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   // all global loads first (K, the log decays and beta), one round trip
   RowTile<T, DK> rk;
   RowScales<RowTile<T, DK>> fk;  // raw keys: row scales (l2 normalisation)
-  rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
+  const KeyHead kh = key_head(a.HK, a.H, h);
+  rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
   if (a.rk) fk.load(a.rk + seq_idx(sq, r0, h, a.H), (size_t)a.H, nrow);
   float la = 0.f, bt = 0.f, rkt = 1.f;
   if (tid < C) {
     const size_t ti = seq_idx(sq, r0 + (tid < nrow ? tid : nrow - 1), h, a.H);
     la = a.logalpha[ti];
+    // a reset: e^-104 is already 0 in fp32, and the sums stay finite where it is -inf
+    if (a.HK && la < -104.f) la = -104.f;
     bt = a.beta[ti];
     if (a.rk) rkt = a.rk[ti];
   }
@@ -79,13 +82,34 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   rk.store(sK, LDQ);
   if (tid < C) {
     float x = tid < nrow ? la : 0.f;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const float y = __shfl_up(x, off);
-      if (tid >= off) x += y;
-    }
+    float toC;  // gamma_C - gamma_j
     bt = tid < nrow ? bt : 0.f;
-    const float gC = __shfl(x, C - 1);
+    float gC;
+    if (a.HK) {
+      // the plain rule's final state is good to fp32: after resets |gamma| is large
+      // against the differences that the decays are formed from, so they are taken
+      // of 64-bit sums (a head and a tail in fp32)
+      double xd = x;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const double y = __shfl_up(xd, off);
+        if (tid >= off) xd += y;
+      }
+      const double gd = __shfl(xd, C - 1);
+      x = (float)xd;
+      toC = (float)(gd - xd);
+      gC = (float)gd;
+      sGamLo[tid] = (float)(xd - (double)x);
+    } else {
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const float y = __shfl_up(x, off);
+        if (tid >= off) x += y;
+      }
+      gC = __shfl(x, C - 1);
+      toC = gC - x;
+      sGamLo[tid] = 0.f;
+    }
     sGam[tid] = x;
     sBeta[tid] = bt;
     float* cf = a.gam + ((size_t)bh * N + ci) * 5 * C + tid;
@@ -94,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     // row's l2 normalisation)
     cf[C] = bt * __expf(x) * rkt;   // beta_j e^{gamma_j}
     cf[2 * C] = bt;                 // beta_j
-    cf[3 * C] = __expf(gC - x) * rkt;  // e^{gamma_C - gamma_j}
+    cf[3 * C] = __expf(toC) * rkt;  // e^{gamma_C - gamma_j}
     cf[4 * C] = __expf(gC);         // e^{gamma_C}
   }
   __syncthreads();
@@ -122,11 +146,12 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     // select discards it
     const f32x4 gi = *reinterpret_cast<const f32x4*>(sGam + 16 * I + 4 * g4);
     const f32x4 bi = *reinterpret_cast<const f32x4*>(sBeta + 16 * I + 4 * g4);
-    const float gj = sGam[16 * J + c16];
+    const f32x4 gil = *reinterpret_cast<const f32x4*>(sGamLo + 16 * I + 4 * g4);
+    const float gj = sGam[16 * J + c16], gjl = sGamLo[16 * J + c16];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * I + 4 * g4 + r, j = 16 * J + c16;
-      const float v = bi[r] * __expf(gi[r] - gj) * acc[s3][r];
+      const float v = bi[r] * __expf((gi[r] - gj) + (gil[r] - gjl)) * acc[s3][r];
       sA[i * LDA + j] = j < i ? v : 0.f;
     }
   }
@@ -176,6 +201,14 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     if ((lc >> 4) > (i >> 4)) lo = zero4();  // above the diagonal blocks
     if (((lc + 16) >> 4) > (i >> 4)) hi = zero4();
     store_acc_pair(Tout + i * C + 8 * q, lo, hi);
+    if (a.TmLo) {  // what the rounding of Tm left
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lo[e] -= f32(to<T>(lo[e]));
+        hi[e] -= f32(to<T>(hi[e]));
+      }
+      store_acc_pair(static_cast<T*>(a.TmLo) + ((size_t)bh * N + ci) * C * C + i * C + 8 * q, lo, hi);
+    }
   }
 }
 
@@ -223,6 +256,7 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
   const int v = v0 + vs;
   const int c0 = hq * DKH;          // first key feature of this wave
   const int b = bh / a.H, h = bh % a.H;
+  const KeyHead kh = key_head(a.HK, a.H, h);
   const Seq sq = seq_of(a.cu, b, a.T);
   const int NL = (sq.len + C - 1) / C;  // chunks walked (a packed sequence's own)
   const T* k = static_cast<const T*>(a.k);
@@ -252,7 +286,7 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
   auto prefetch = [&](Stage& sg, int ci) {
     const int r0 = ci * C;
     const int nrow = (sq.len - r0) < C ? (sq.len - r0) : C;
-    sg.rk.load(k + seq_off(sq, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
+    sg.rk.load(k + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     sg.rt.load(Tg + ((size_t)bh * N + ci) * C * C, (size_t)C, C);
     sg.rv.load(vin + seq_off(sq, r0, h, a.H, a.dv) + v0, (size_t)a.H * a.dv, nrow);
     if (tid < C) {
@@ -444,7 +478,9 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id();
   const int g4 = l >> 4, c16 = l & 15;
   const int vg = w % NVG, ig = NIG == 1 ? 0 : w / NVG;  // (uniform: no lane-masked branch on the tile)
-  const size_t gstride = (size_t)a.H * DK;
+  const KeyHead kh = key_head(a.HK, a.H, h);
+  const size_t gstride = (size_t)kh.H * DK;
+  const Seq sqq = a.HK ? sq : padded_rows(sq, b, a.T);  // q_clean: the workspace's padded rows
   T* o = static_cast<T*>(a.o);
 
   Frag<T> sfr[VPW][NK];
@@ -454,9 +490,8 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
     const bool carry = CARRY && ci + 1 < ce;
     {
       RowTile<T, DK, kOutThreads> rq, rk;
-      rq.load(static_cast<const T*>(a.qc) + seq_off(padded_rows(sq, b, a.T), r0, h, a.H, DK), gstride,
-              nrow);  // q_clean: the workspace's padded rows
-      rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, h, a.H, DK), gstride, nrow);
+      rq.load(static_cast<const T*>(a.qc) + seq_off(sqq, r0, kh.h, kh.H, DK), gstride, nrow);
+      rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), gstride, nrow);
       const float* gm = a.gam + ((size_t)bh * N + ci) * 5 * C;
       if (tid < C) sGam[tid] = gm[tid];
       if (a.rk && tid < C) sRk[tid] = a.rk[seq_idx(sq, r0 + (tid < nrow ? tid : nrow - 1), h, a.H)];

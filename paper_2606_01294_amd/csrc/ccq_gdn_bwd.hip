@@ -59,8 +59,9 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
   {
     RowTile<T, DK> rq, rk;
     RowTile<T, C> rt;
-    rq.load(static_cast<const T*>(a.qc) + seq_off(sp, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
-    rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
+    const KeyHead kh = key_head(a.HK, a.H, h);
+    rq.load(static_cast<const T*>(a.qc) + seq_off(a.HK ? sq : sp, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
+    rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     rt.load(static_cast<const T*>(a.Tm) + cidx * C * C, (size_t)C, C);
     if (tid < C) sGam[tid] = a.gam[cidx * 5 * C + tid];
     rq.store(sQ, LDQ);
@@ -145,6 +146,8 @@ void gdn_dstate_kernel(const GdnDstateArgs a) {
   const int v0 = (lb % nvt) * BVS;
   const int b = bh / a.H, h = bh % a.H;
   const Seq sq = seq_of(a.cu, b, a.T), sp = padded_rows(sq, b, a.T);
+  const KeyHead kh = key_head(a.HK, a.H, h);
+  const Seq sqq = a.HK ? sq : sp;
   const int NL = (sq.len + C - 1) / C;  // chunks walked (a packed sequence's own)
   const int tid = threadIdx.x, w = wave_id(), l = lane_id();
   const int pr = w / NH, hq = w % NH;
@@ -181,8 +184,8 @@ void gdn_dstate_kernel(const GdnDstateArgs a) {
   auto prefetch_kq = [&](int ci) {
     const int r0 = ci * C;
     const int nrow = (sq.len - r0) < C ? (sq.len - r0) : C;
-    st.rk.load(k + seq_off(sq, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
-    st.rq.load(qc + seq_off(sp, r0, h, a.H, DK), (size_t)a.H * DK, nrow);
+    st.rk.load(k + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
+    st.rq.load(qc + seq_off(sqq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
   };
   auto prefetch = [&](int ci) {
     const int r0 = ci * C;
@@ -349,7 +352,7 @@ void gdn_dstate_kernel(const GdnDstateArgs a) {
 // eight waves (NW = 8) the two waves of a stripe split its key-channel tiles
 // and its C x C tiles (J of the same parity as the wave's half); their
 // per-row sums meet through LDS.
-template <typename T, int DK, int BV, int NW>
+template <typename T, int DK, int BV, int NW, bool PLAIN>
 __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdArgs a) {
   constexpr int C = kChunk, NT = 64 * NW;
   constexpr int HW = NW / 4;  // waves per stripe
@@ -387,14 +390,16 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   const int g4 = l >> 4, c16 = l & 15;
   const size_t cidx = (size_t)bh * N + ci;
   const size_t gsk = (size_t)a.H * DK, gsv = (size_t)a.H * a.dv;
+  const KeyHead kh = PLAIN ? key_head(a.HK, a.H, h) : KeyHead{a.H, h};
+  const size_t gsq = (size_t)kh.H * DK;
   const float eC = a.gam[(cidx * 5 + 4) * C];
 
   // ---- phase 1: Q K^T and K K^T (rows of stripe sw, this wave's tiles J <= sw)
   f32x4 QK[NJ], KK[NJ];
   {
     ChunkTile<T, DK, NT> rq, rk;
-    rq.load(static_cast<const T*>(a.qc) + seq_off(sp, r0, h, a.H, DK), gsk, nrow);
-    rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, h, a.H, DK), gsk, nrow);
+    rq.load(static_cast<const T*>(a.qc) + seq_off(PLAIN ? sq : sp, r0, kh.h, kh.H, DK), gsq, nrow);
+    rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), gsq, nrow);
     if (tid < C) {
       sGam[tid] = a.gam[cidx * 5 * C + tid];
       sBeta[tid] = a.gam[(cidx * 5 + 2) * C + tid];
@@ -550,6 +555,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   // Sigma_t q_t for this wave's rows, requested now for the epilogue
   const size_t rowoff = seq_off(sp, r0, h, a.H, DK);
   float cr[NTW][4];
+  if constexpr (!PLAIN)
 #pragma unroll
   for (int ct = 0; ct < NTW; ++ct)
 #pragma unroll
@@ -623,7 +629,15 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       dot1[r] += G1[ct][r] * qv;
       dot2[r] += G2[ct][r] * kv;
       dot3[r] += G3[ct][r] * kv;
-      if (i < nrow) {
+      if (PLAIN && i < nrow && a.HK == a.H) {
+        const size_t off = seq_off(sq, r0 + i, h, a.H, DK) + c;
+        dqc_io[off] = to<T>(dq);
+        static_cast<T*>(a.dk_io)[off] = to<T>(dk);
+      } else if (PLAIN && i < nrow) {
+        const size_t off = rowoff + i * (int)gsk + c;
+        a.dqc[off] = dq;
+        a.dk_bb[off] = dk;
+      } else if (!PLAIN && i < nrow) {
         const size_t off = rowoff + i * (int)gsk + c;
         a.dqc[off] = dq;
         dqc_io[off] = to<T>(dq);
@@ -683,8 +697,13 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         xt += i < nrow ? sDec[i] * d3[r] : 0.f;
         if (i < nrow) {
           const size_t ti = seq_idx(sq, r0 + i, h, a.H);
-          a.dbeta[ti] = sRV[i] - G * d2[r] + ra[r];
-          a.dlam[ti] = dlam[r];
+          const float dbt = sRV[i] - G * d2[r] + ra[r];
+          if constexpr (PLAIN) {
+            static_cast<T*>(a.dbeta_io)[ti] = to<T>(dbt);
+          } else {
+            a.dbeta[ti] = dbt;
+            a.dlam[ti] = dlam[r];
+          }
         }
       }
     }
@@ -708,7 +727,11 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       const float y = __shfl_down(x, off);
       if (l + off < 64) x += y;
     }
-    if (l < nrow) a.dlogalpha[seq_idx(sq, r0 + l, h, a.H)] = x;
+    if (l < nrow) {
+      const size_t ti = seq_idx(sq, r0 + l, h, a.H);
+      if constexpr (PLAIN) static_cast<T*>(a.dla_io)[ti] = to<T>(x);
+      else a.dlogalpha[ti] = x;
+    }
   }
 }
 
@@ -745,7 +768,10 @@ hipError_t run_bwd_chunk(const GdnBwdArgs& a, hipStream_t st) {
   const int nblk = a.B * a.H * ((a.T + kChunk - 1) / kChunk);
   if (nblk == 0) return hipSuccess;
   constexpr int BV = 32;
-  hipLaunchKernelGGL((gdn_bwd_chunk_kernel<T, DK, BV, NW>), dim3(nblk), dim3(64 * NW), 0, st, a);
+  if (a.HK)
+    hipLaunchKernelGGL((gdn_bwd_chunk_kernel<T, DK, BV, NW, true>), dim3(nblk), dim3(64 * NW), 0, st, a);
+  else
+    hipLaunchKernelGGL((gdn_bwd_chunk_kernel<T, DK, BV, NW, false>), dim3(nblk), dim3(64 * NW), 0, st, a);
   return hipGetLastError();
 }
 }  // namespace

@@ -133,6 +133,10 @@ struct TriArgs {
   // coefficients beta e^gamma and e^{gamma_C - gamma} that multiply key rows
   // in the state pass and the output kernel's carry are stored times rk
   const float* rk = nullptr;
+  // the plain rule: query/key heads that the H value heads share (0: H of them),
+  // and the tail of Tm (Tm is then the head of a bf16 pair), or null
+  int HK = 0;
+  void* TmLo = nullptr;
 };
 
 // Gated DeltaNet state recurrence (sequential over chunks): writes the
@@ -153,6 +157,8 @@ struct GdnArgs {
   int B, T, H, dk, dv;
   int sstride = 1;
   const int* cu = nullptr;  // as TriArgs
+  int HK = 0;               // as TriArgs
+  const void* TmLo = nullptr;
 };
 
 // Gated DeltaNet output, one workgroup per group of `group` chunks (the
@@ -169,6 +175,7 @@ struct GdnOutArgs {
   int group = 1;
   const int* cu = nullptr;  // as TriArgs
   const float* rk = nullptr;  // key row scales (the scores'; the carry's come with the coefficients)
+  int HK = 0;  // as TriArgs; if set, qc holds the caller's queries (its rows, HK heads)
 };
 
 // ---- training step (CCQ-GLA backward) ----
@@ -234,6 +241,7 @@ struct GdnPrepArgs {
   void* TmT;             // [B*H, N, C, C] io
   int B, T, H, dk, dv;
   const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
+  int HK = 0;               // as GdnOutArgs
 };
 
 // Reverse scan of the state adjoint D = dS_{r+1} over the chunks of one head:
@@ -250,6 +258,7 @@ struct GdnDstateArgs {
   int B, T, H, dk, dv;
   float scale;
   const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
+  int HK = 0;               // as GdnOutArgs
 };
 
 // Chunk-parallel Gated DeltaNet gradients given S_r, U, dS_{r+1} and dR.
@@ -271,6 +280,36 @@ struct GdnBwdArgs {
   int B, T, H, dk, dv;
   float scale;
   const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
+  // the plain rule (HK > 0, as GdnOutArgs): the gates' gradients in io dtype;
+  // with HK = H dq and dk to the caller's rows in io dtype (dqc_io, dk_io), else
+  // every value head's in fp32 to the workspace (dqc, dk_bb); no corr, no dlam
+  int HK = 0;
+  void* dk_io = nullptr;
+  void* dla_io = nullptr;
+  void* dbeta_io = nullptr;
+};
+
+// ---- the gated delta rule without the contraction ----
+struct DeltaStepArgs {
+  const void* q;          // [B,T,HK,dk] io
+  const void* k;          // [B,T,HK,dk] io
+  const void* v;          // [B,T,HV,dv] io
+  const float* logalpha;  // [B,T,HV]
+  const float* beta;      // [B,T,HV]
+  float* S;               // [B,HV,dv,dk] fp32, in place
+  void* o;                // [B,T,HV,dv] io
+  int B, T, HK, HV, dk, dv;
+  float scale;
+};
+// dq and dk of every value head (fp32, padded [B,T,HV,dk]) summed over the value
+// heads of a query/key head, to [B,T,HK,dk] (or packed rows) io.
+struct HeadSumArgs {
+  const float* dq;
+  const float* dk_in;
+  void* dq_out;
+  void* dk_out;
+  int B, T, HK, HV, dk;
+  const int* cu = nullptr;
 };
 
 // ---- recurrent decode (one token per sequence, cache updated in place) ----
@@ -307,6 +346,54 @@ struct PrepArgs {
   // instead of the normalised rows: the row scales 1 / max(|x|, 1e-12) [B,T,H]
   float* rq = nullptr;
   float* rk = nullptr;
+};
+
+// ---- norm of the head outputs, short convolution (memory-bound operators) ----
+enum { kNormGroup = 0, kNormRms = 1, kNormL2 = 2 };
+enum { kActNone = 0, kActSilu = 1, kActSigmoid = 2 };
+struct NormArgs {
+  const void* x;         // [rows, G, D] io, row pitch ldx elements
+  const float* w;        // [G, D], or [D] (shared), or null (ones)
+  const float* bias;     // as w, or null (zeros)
+  const void* gate;      // [rows, G, D] io, row pitch ldg, or null
+  void* y;               // forward: [rows, G, D] io
+  const void* dy;        // backward: [rows, G, D] io
+  void* dx;              // [rows, G, D] io
+  void* dgate;           // [rows, G, D] io (with a gate)
+  float* part;           // backward workspace: norm_part_rows rows of sums of dw (and db), or null
+  long long rows, ldx, ldg;
+  int G, D;
+  int kind, act, shared;
+  float eps;
+  long long slots = 0;   // set by launch_norm
+};
+struct ConvArgs {
+  const void* x;         // [B,T,C] io (packed: [rows, C]), token pitch ldx elements; the step: [B, C]
+  const float* w;        // [C, W]
+  const float* bias;     // [C] or null
+  const void* state0;    // [B, W-1, C] io or null: the inputs before the first token, oldest first
+  void* y;               // [B,T,C] io
+  void* stateT;          // [B, W-1, C] io or null: the last W-1 inputs (the step: in place)
+  const void* dy;        // backward
+  const void* dstateT;   // [B, W-1, C] io or null
+  void* dx;
+  void* dstate0;         // [B, W-1, C] io or null
+  float* part;           // backward workspace: conv_part_rows rows of (W + 1) C sums, or null
+  int B, T, C, act;
+  long long ldx;
+  const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
+  int runs = 0;          // runs of tokens per sequence, set by launch_conv
+};
+enum class ConvCall { kFwd, kBwd, kStep };
+// Sums of the columns of part [rows, cols]: columns below `first` to out0, the
+// others to out1; with taps, out0 column j C + c goes to out0[c taps + j].
+struct ColsumArgs {
+  const float* part;
+  long long rows;
+  int cols, first;
+  float* out0;
+  float* out1;
+  int taps, C;
 };
 
 // Each launcher returns hipSuccess or the launch error.  is_bf16 selects the
@@ -365,6 +452,9 @@ hipError_t launch_gdn_tri(const TriArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_gdn_state(const GdnArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_gdn_state_roles(const GdnArgs& a, hipStream_t st);  // bf16, dk = 128 or 256
 hipError_t launch_gdn_out(const GdnOutArgs& a, bool is_bf16, hipStream_t st);
+hipError_t launch_delta_state(const GdnArgs& a, hipStream_t st);  // bf16
+hipError_t launch_delta_step(const DeltaStepArgs& a, bool is_bf16, hipStream_t st);
+hipError_t launch_head_sum(const HeadSumArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_copy_or_zero(float* dst, const float* src, size_t n, hipStream_t st);
 
 hipError_t launch_gla_dstate(const DstateArgs& a, bool is_bf16, bool gate_bf16, hipStream_t st);
@@ -381,7 +471,15 @@ bool decode_split(long long bh, int dk, int dv);  // two launches over 16-row bl
 hipError_t launch_prep(const PrepArgs& a, bool is_bf16, hipStream_t st);
 bool prep_supported(int H, int dk);
 
+hipError_t launch_norm(NormArgs a, bool is_bf16, bool bwd, hipStream_t st);
+long long norm_part_rows(long long rows, int G, int D, int shared);
+hipError_t launch_conv(const ConvArgs& a, int W, ConvCall call, bool is_bf16, hipStream_t st);
+long long conv_part_rows(int B, int T);
+hipError_t launch_colsum(const ColsumArgs& a, hipStream_t st);
+
 // Supported-shape predicates (used by validation before any launch).
+bool norm_supported(int D);
+bool conv_supported(int B, int T, int C, int W);
 bool clean_supported(int dk, bool is_bf16);
 bool gla_supported(int dk, int dv, bool is_bf16);
 // Chunks per output workgroup of the GLA forward (1: one chunk each).

@@ -1,0 +1,355 @@
+// ccq_norm.hip -- group norm of the mixer's head outputs with an activation,
+// channels last: forward and backward.
+//
+// x is [rows, G, D]: a token's G heads of D channels, each normalised on its own
+// (an item; statistics over tokens would look ahead).  With n the normalisation,
+//   group  n = (x - m) r,  m = mean x,  r = (mean (x - m)^2 + eps)^-1/2
+//   rms    n = x r,        r = (mean x^2 + eps)^-1/2
+//   l2     n = x r,        r = (sum x^2 + eps)^-1/2
+//   z = n w + b,   y = z act(gate)  with a gate,  y = act(z)  without.
+// Backward, with c = 1 / D (1 for l2) and h = dz w:
+//   dz = dy act(gate), dgate = dy z act'(gate)   or   dz = dy act'(z);
+//   dw = sum dz n,  db = sum dz;  dx = r (h - [group: mean h] - n c sum(h n)).
+//
+// Both directions read every tensor once and keep an item in registers between
+// its sums and its use, so HBM bounds them.  An item is held by LPI consecutive
+// lanes (a power of two, up to a wave; a workgroup above 1024 channels), NV vectors
+// of eight channels each.  A slot of LPI lanes takes the items s, s + NS, ... with
+// NS a multiple of G: its head never changes, so the weights are read once and the
+// backward sums dw and db in registers, over all of a slot's rows.  The sums of the
+// slots (of the workgroups, where the heads share one weight) meet in a second
+// kernel in a fixed order: no atomics, the same bits every time.
+// Sums, statistics and the affine part are fp32; what is stored is rounded once.
+#include "ccq_device.h"
+#include "ccq_kernels.h"
+#include "ccq_pointwise.h"
+
+namespace ccq {
+
+namespace {
+constexpr int kNormThreads = 256;
+
+// Sum over the LPI lanes (or, for LPI = 256, the workgroup) that hold an item.
+template <int LPI>
+__device__ __forceinline__ float item_sum(float x, float* red) {
+  if constexpr (LPI >= 2) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x041F));
+  if constexpr (LPI >= 4) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x081F));
+  if constexpr (LPI >= 8) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x101F));
+  if constexpr (LPI >= 16) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x201F));
+  if constexpr (LPI >= 32) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x401F));
+  if constexpr (LPI >= 64) x += __shfl_xor(x, 32);
+  if constexpr (LPI > 64) {  // four waves; the array is free again after the second barrier
+    if (lane_id() == 0) red[wave_id()] = x;
+    __syncthreads();
+    x = (red[0] + red[1]) + (red[2] + red[3]);
+    __syncthreads();
+  }
+  return x;
+}
+
+// The lane's channels of one item: vector u is channels 8 (j + LPI u) ..
+template <int LPI, int NV>
+struct ItemCols {
+  int j, nvec;  // lane within the item, vectors per item
+  __device__ __forceinline__ bool has(int u) const { return j + LPI * u < nvec; }
+  __device__ __forceinline__ int col(int u) const { return 8 * (j + LPI * u); }
+};
+
+// n and r of one item, in place of x.
+template <int LPI, int NV>
+__device__ __forceinline__ float normalise(float (&x)[NV][8], const ItemCols<LPI, NV>& ic, const NormArgs& a, float* red) {
+  const float inv = 1.f / (float)a.D;
+  if (a.kind == kNormGroup) {
+    float s = 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += x[u][e];
+    const float m = item_sum<LPI>(s, red) * inv;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[u][e] = ic.has(u) ? x[u][e] - m : 0.f;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += x[u][e] * x[u][e];
+  s = item_sum<LPI>(s, red);
+  const float r = 1.f / sqrtf(s * (a.kind == kNormL2 ? 1.f : inv) + a.eps);
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[u][e] *= r;
+  return r;
+}
+
+template <int LPI, int NV>
+__device__ __forceinline__ void load_affine(float (&w)[NV][8], const float* p, int head, float other, const ItemCols<LPI, NV>& ic,
+                                            const NormArgs& a) {
+  const float* q = p + (a.shared ? 0 : (size_t)head * a.D);
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[u][e] = p && ic.has(u) ? q[ic.col(u) + e] : other;
+}
+}  // namespace
+
+template <typename T, int LPI, int NV, bool GATE>
+__global__ __launch_bounds__(kNormThreads) void norm_fwd_kernel(const NormArgs a) {
+  typedef Vec8<T> V;
+  constexpr int U = NV == 1 ? 2 : 1;  // items in flight
+  __shared__ float red[4];
+  const long long s = ((long long)blockIdx.x * kNormThreads + threadIdx.x) / LPI;
+  if (s >= a.slots) return;  // whole slots (LPI = 256: the workgroup)
+  const ItemCols<LPI, NV> ic{(int)(threadIdx.x % LPI), a.D / 8};
+  const int head = (int)(s % a.G);
+  const long long step = a.slots / a.G;
+  const T* x = static_cast<const T*>(a.x) + (size_t)head * a.D;
+  const T* gate = static_cast<const T*>(a.gate) + (size_t)head * a.D;
+  T* y = static_cast<T*>(a.y) + (size_t)head * a.D;
+  float w[NV][8], b[NV][8];
+  load_affine(w, a.w, head, 1.f, ic, a);
+  load_affine(b, a.bias, head, 0.f, ic, a);
+  for (long long row = s / a.G; row < a.rows; row += U * step) {
+    typename V::raw rx[U][NV], rg[U][NV];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const long long rr = row + i * step < a.rows ? row + i * step : row;
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+        if (ic.has(u)) {
+          rx[i][u] = V::load(x + (size_t)rr * a.ldx + ic.col(u));
+          if constexpr (GATE) rg[i][u] = V::load(gate + (size_t)rr * a.ldg + ic.col(u));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const long long rr = row + i * step;
+      if (rr >= a.rows) break;
+      float v[NV][8];
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = ic.has(u) ? V::get(rx[i][u], e) : 0.f;
+      normalise<LPI, NV>(v, ic, a, red);
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+        if (ic.has(u)) {
+          float o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z = v[u][e] * w[u][e] + b[u][e];
+            if constexpr (GATE) o[e] = z * Act<T>::value(a.act, V::get(rg[i][u], e));
+            else o[e] = Act<T>::value(a.act, z);
+          }
+          V::store(y + (size_t)rr * a.G * a.D + ic.col(u), o);
+        }
+    }
+  }
+}
+
+// dw and db of a slot's rows go to partial row s / G, columns head D + .. (or,
+// with one weight for all heads, the workgroup's sum to row blockIdx.x), db
+// behind all of dw.
+template <typename T, int LPI, int NV, bool GATE>
+__global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a) {
+  typedef Vec8<T> V;
+  constexpr int SPW = LPI < 64 ? 64 / LPI : 1;  // slots per wave
+  __shared__ float red[4];
+  const long long s = ((long long)blockIdx.x * kNormThreads + threadIdx.x) / LPI;
+  const ItemCols<LPI, NV> ic{(int)(threadIdx.x % LPI), a.D / 8};
+  const int head = (int)(s % a.G);
+  const long long step = a.slots / a.G;
+  const T* x = static_cast<const T*>(a.x) + (size_t)head * a.D;
+  const T* gate = static_cast<const T*>(a.gate) + (size_t)head * a.D;
+  const T* dy = static_cast<const T*>(a.dy) + (size_t)head * a.D;
+  T* dx = static_cast<T*>(a.dx) + (size_t)head * a.D;
+  T* dgate = static_cast<T*>(a.dgate) + (size_t)head * a.D;
+  const size_t ldy = (size_t)a.G * a.D;
+  const float c = a.kind == kNormL2 ? 1.f : 1.f / (float)a.D;
+  float w[NV][8], b[NV][8], dw[NV][8], db[NV][8];
+  load_affine(w, a.w, head, 1.f, ic, a);
+  load_affine(b, a.bias, head, 0.f, ic, a);
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[u][e] = db[u][e] = 0.f;
+
+  // the next item's tensors are requested while one is worked on
+  typename V::raw rx[NV], rg[NV], rd[NV];
+  auto load = [&](long long row) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if (ic.has(u)) {
+        rx[u] = V::load(x + (size_t)row * a.ldx + ic.col(u));
+        if constexpr (GATE) rg[u] = V::load(gate + (size_t)row * a.ldg + ic.col(u));
+        rd[u] = V::load(dy + (size_t)row * ldy + ic.col(u));
+      }
+  };
+  const long long first = s < a.slots ? s / a.G : a.rows;  // (slots behind the last one: no rows)
+  if (first < a.rows) load(first);
+  for (long long row = first; row < a.rows; row += step) {
+    float n[NV][8], g[NV][8], d[NV][8];
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        n[u][e] = ic.has(u) ? V::get(rx[u], e) : 0.f;
+        if constexpr (GATE) g[u][e] = ic.has(u) ? V::get(rg[u], e) : 0.f;
+        d[u][e] = ic.has(u) ? V::get(rd[u], e) : 0.f;
+      }
+    if (row + step < a.rows) load(row + step);
+    const float r = normalise<LPI, NV>(n, ic, a, red);
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      float og[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float z = n[u][e] * w[u][e] + b[u][e];
+        float av, ad;
+        Act<T>::both(a.act, GATE ? g[u][e] : z, av, ad);
+        float dz;
+        if constexpr (GATE) {
+          og[e] = d[u][e] * z * ad;
+          dz = d[u][e] * av;
+        } else {
+          dz = d[u][e] * ad;
+        }
+        dw[u][e] += dz * n[u][e];
+        db[u][e] += dz;
+        const float h = dz * w[u][e];
+        d[u][e] = h;
+        s0 += h;
+        s1 += h * n[u][e];
+      }
+      if constexpr (GATE)
+        if (ic.has(u)) V::store(dgate + (size_t)row * ldy + ic.col(u), og);
+    }
+    s1 = item_sum<LPI>(s1, red) * c;
+    s0 = a.kind == kNormGroup ? item_sum<LPI>(s0, red) * c : 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if (ic.has(u)) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = r * (d[u][e] - s0 - n[u][e] * s1);
+        V::store(dx + (size_t)row * ldy + ic.col(u), o);
+      }
+  }
+
+  if (!a.part) return;
+  const bool bias = a.bias != nullptr;
+  const size_t cols = (size_t)(a.shared ? 1 : a.G) * a.D;  // of dw
+  const size_t pitch = cols * (bias ? 2 : 1);
+  if (!a.shared) {
+    if (s >= a.slots) return;
+    float* out = a.part + (size_t)(s / a.G) * pitch + (size_t)head * a.D;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if (ic.has(u))
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          out[ic.col(u) + e] = dw[u][e];
+          if (bias) out[cols + ic.col(u) + e] = db[u][e];
+        }
+    return;
+  }
+  // one weight for all heads: the workgroup's slots are summed first
+  __shared__ float buf[LPI > 64 ? 1 : 4][LPI > 64 ? 1 : LPI * NV * 8];
+  float* out = a.part + (size_t)blockIdx.x * pitch;
+  for (int q = 0; q < (bias ? 2 : 1); ++q) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float t = q ? db[u][e] : dw[u][e];
+        if constexpr (SPW > 1)
+#pragma unroll
+          for (int off = LPI; off < 64; off <<= 1) t += __shfl_xor(t, off);
+        if constexpr (LPI > 64) {
+          if (ic.has(u)) out[q * cols + ic.col(u) + e] = t;
+        } else if (lane_id() < LPI) {
+          buf[wave_id()][ic.j * 8 + LPI * 8 * u + e] = t;
+        }
+      }
+    if constexpr (LPI <= 64) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < a.D; i += kNormThreads)
+        out[q * cols + i] = (buf[0][i] + buf[1][i]) + (buf[2][i] + buf[3][i]);
+      __syncthreads();
+    }
+  }
+}
+
+namespace {
+int norm_lanes(int D) {  // lanes that hold an item: 8 channels each, a power of two
+  const int nvec = D / 8;
+  int l = 1;
+  while (l < nvec && l < 64) l *= 2;
+  return nvec > 128 ? 256 : l;
+}
+
+// Slots: enough waves to fill the chip and no more, so that a slot's weights (and
+// in the backward its sums) serve many rows; always a multiple of G.  Forward: 32
+// waves a compute unit; backward: 16.
+long long norm_slots(long long rows, int G, int lanes, bool bwd) {
+  const long long threads = 256ll * (bwd ? 16 : 32) * 64;
+  long long step = (threads / lanes + G - 1) / G;
+  if (step < 1) step = 1;
+  return (rows < step ? rows : step) * G;
+}
+
+long long norm_blocks(long long slots, int lanes) { return (slots * lanes + kNormThreads - 1) / kNormThreads; }
+
+template <typename T, int LPI, int NV>
+hipError_t run_norm(const NormArgs& a, bool bwd, hipStream_t st) {
+  const dim3 grid((unsigned)norm_blocks(a.slots, LPI)), block(kNormThreads);
+  if (!bwd) {
+    if (a.gate) hipLaunchKernelGGL((norm_fwd_kernel<T, LPI, NV, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, LPI, NV, false>), grid, block, 0, st, a);
+  } else {
+    if (a.gate) hipLaunchKernelGGL((norm_bwd_kernel<T, LPI, NV, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((norm_bwd_kernel<T, LPI, NV, false>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_dispatch(const NormArgs& a, bool bwd, hipStream_t st) {
+  switch (norm_lanes(a.D)) {
+    case 1: return run_norm<T, 1, 1>(a, bwd, st);
+    case 2: return run_norm<T, 2, 1>(a, bwd, st);
+    case 4: return run_norm<T, 4, 1>(a, bwd, st);
+    case 8: return run_norm<T, 8, 1>(a, bwd, st);
+    case 16: return run_norm<T, 16, 1>(a, bwd, st);
+    case 32: return run_norm<T, 32, 1>(a, bwd, st);
+    case 64:
+      if (a.D <= 512) return run_norm<T, 64, 1>(a, bwd, st);
+      return run_norm<T, 64, 2>(a, bwd, st);
+    case 256:
+      if (a.D <= 2048) return run_norm<T, 256, 1>(a, bwd, st);
+      if (a.D <= 4096) return run_norm<T, 256, 2>(a, bwd, st);
+      return run_norm<T, 256, 4>(a, bwd, st);
+  }
+  return hipErrorInvalidValue;
+}
+}  // namespace
+
+bool norm_supported(int D) { return D >= 8 && D <= 8192 && D % 8 == 0; }
+
+// Rows of partial sums of dw (and db) that the backward leaves for colsum.
+long long norm_part_rows(long long rows, int G, int D, int shared) {
+  const int lanes = norm_lanes(D);
+  const long long slots = norm_slots(rows, G, lanes, true);
+  return shared ? norm_blocks(slots, lanes) : slots / G;
+}
+
+hipError_t launch_norm(NormArgs a, bool is_bf16, bool bwd, hipStream_t st) {
+  a.slots = norm_slots(a.rows, a.G, norm_lanes(a.D), bwd);
+  return is_bf16 ? norm_dispatch<bf16_t>(a, bwd, st) : norm_dispatch<float>(a, bwd, st);
+}
+
+}  // namespace ccq

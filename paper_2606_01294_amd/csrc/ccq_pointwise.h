@@ -1,0 +1,57 @@
+// ccq_pointwise.h -- device helpers of the memory-bound operators around the
+// recurrence (convolution, norm): vectors of channels, activations, and sums of
+// the rows of a matrix of partial sums.
+#pragma once
+#include "ccq_device.h"
+#include "ccq_kernels.h"
+
+namespace ccq {
+
+// Eight (N) consecutive channels of one row, 16-byte loads and stores.
+template <typename T, int N = 8>
+struct VecN {
+  typedef T raw __attribute__((ext_vector_type(N)));
+  static __device__ __forceinline__ raw load(const T* p) { return *reinterpret_cast<const raw*>(p); }
+  static __device__ __forceinline__ float get(const raw& v, int e) { return static_cast<float>(v[e]); }
+  static __device__ __forceinline__ void store(T* p, const float (&x)[N]) {
+    raw v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = static_cast<T>(x[e]);
+    *reinterpret_cast<raw*>(p) = v;
+  }
+};
+template <typename T> using Vec8 = VecN<T, 8>;
+
+// act(z) and act'(z): none, silu (z sigmoid z), sigmoid.  bf16 io takes the
+// hardware's exponential and reciprocal (about 1e-6 relative, far below the
+// 2^-9 of the rounding on store); fp32 io the full-precision ones.  exp(-z)
+// overflows to infinity for z < -88, where sigmoid is then an exact 0.
+template <typename T>
+struct Act {
+  static __device__ __forceinline__ float sigmoid(float z) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    else return 1.f / (1.f + expf(-z));
+  }
+  static __device__ __forceinline__ float value(int act, float z) {
+    if (act == kActNone) return z;
+    const float s = sigmoid(z);
+    return act == kActSilu ? z * s : s;
+  }
+  static __device__ __forceinline__ void both(int act, float z, float& v, float& d) {
+    if (act == kActNone) {
+      v = z;
+      d = 1.f;
+      return;
+    }
+    const float s = sigmoid(z);
+    if (act == kActSilu) {
+      v = z * s;
+      d = s * (1.f + z * (1.f - s));
+    } else {
+      v = s;
+      d = s * (1.f - s);
+    }
+  }
+};
+
+}  // namespace ccq

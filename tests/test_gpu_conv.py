@@ -1,0 +1,194 @@
+"""Short causal convolution (ccq_conv_*) against the sum itself in 64 bits, with autograd for its
+gradients, and against differences.
+
+Tolerance, per element: half a step of the stored type (2^-8 of the value for bf16, 2^-24 for
+fp32) plus the fp32 work before it.  z is W + 1 products, each off by 2^-24 of its size, and the
+activation's derivative is at most 1.1, so that part is below 2 (W + 2) 2^-24 M with M the sum of
+the terms' sizes; bf16 io evaluates the activation by the hardware's exponential and reciprocal,
+2^-20 relative for the |z| < 16 of these inputs.  A gradient's dz has the same error, W terms of it
+are summed: 64 2^-24 M covers fp32, 2^-16 M bf16.  dw and dbias are fp32 sums over all tokens:
+their terms carry the error of dz (2^-18 with bf16 io) and the summation adds, in partial sums of
+at most 2^12 terms, 2^-24 12 of the terms' sizes: 2^-17 M."""
+import pytest
+import torch
+
+from paper_2606_01294_amd import ccq
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+ACTS = {"none": 0, "silu": 1, "sigmoid": 2}
+
+
+def act64(name, z):
+    return {"none": z, "silu": z * torch.sigmoid(z), "sigmoid": torch.sigmoid(z)}[name]
+
+
+def reference(seqs, w, bias, state0, act):
+    """seqs: list of [n, C] float64; returns ys, final states, and the sizes of z's terms."""
+    ys, ends, mags = [], [], []
+    C, W = w.shape
+    for b, x in enumerate(seqs):
+        head = x.new_zeros(W - 1, C) if state0 is None else state0[b]
+        e = torch.cat([head, x])
+        n = x.shape[0]
+        z = sum(w[:, j] * e[j:j + n] for j in range(W))
+        m = sum(w[:, j].abs() * e[j:j + n].abs() for j in range(W))
+        if bias is not None:
+            z, m = z + bias, m + bias.abs()
+        ys.append(act64(act, z))
+        ends.append(e[n:])
+        mags.append(m)
+    return ys, ends, mags
+
+
+def make(lens, C, W, dt, bias, state, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    x = r(sum(lens), C).to(dt)
+    w = r(C, W) * W ** -0.5
+    b = 0.1 * r(C) if bias else None
+    s0 = r(len(lens), W - 1, C).to(dt) if state else None
+    dy = r(sum(lens), C).to(dt)
+    dsT = r(len(lens), W - 1, C).to(dt)
+    return x, w, b, s0, dy, dsT
+
+
+def close(got, ref, mag, dt, what):
+    half = {BF: 2.0 ** -8, F32: 2.0 ** -24}[dt]
+    work = {BF: 2.0 ** -16, F32: 64 * 2.0 ** -24}[dt]
+    got = got.detach().double().cpu()
+    bad = (got - ref).abs() > half * ref.abs() + work * mag
+    print(what, "max off", float((got - ref).abs().max()) if got.numel() else 0.0, flush=True)
+    assert got.shape == ref.shape and not bool(bad.any()), (what, int(bad.sum()))
+
+
+CASES = [  # lens (one length for all: padded), C, W, dtype, act, bias, state, packed
+    ([1, 1], 64, 4, BF, "silu", True, True, False),
+    ([2, 2, 2], 8, 4, BF, "silu", True, False, False),
+    ([33, 33], 72, 3, F32, "silu", True, True, False),
+    ([64], 520, 2, BF, "sigmoid", False, True, False),
+    ([300, 300], 640, 4, BF, "silu", True, False, False),
+    ([129], 2056, 4, F32, "none", True, True, False),
+    ([31, 0, 1, 32, 2, 97, 0], 136, 4, BF, "silu", True, True, True),
+    ([0, 3, 0], 16, 3, F32, "silu", False, True, True),
+    ([70, 5, 128], 1024, 4, BF, "silu", True, False, True),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+def test_forward_and_backward(case):
+    lens, C, W, dt, act, bias, state, packed = case
+    x, w, b, s0, dy, dsT = make(lens, C, W, dt, bias, state)
+    leaf = [t.double().requires_grad_() if t is not None else None for t in (x, w, b, s0)]
+    ys, ends, mags = reference(leaf[0].split(lens), leaf[1], leaf[2], leaf[3], act)
+    y, end, mag = torch.cat(ys), torch.stack(ends), torch.cat(mags)
+    names = [n for n, t in zip(("dx", "dw", "dbias", "dstate0"), leaf) if t is not None]
+    ref = dict(zip(names, torch.autograd.grad(
+        [y, end], [t for t in leaf if t is not None], [dy.double(), dsT.double()],
+        allow_unused=True, materialize_grads=True)))
+    cu = torch.tensor([0] + [sum(lens[:i + 1]) for i in range(len(lens))], dtype=torch.int32)
+    d = lambda t: None if t is None else t.cuda()  # noqa: E731
+    kw = dict(bias=d(b), state0=d(s0), act=ACTS[act])
+    if packed:
+        # rows behind the last sequence stay as they are
+        behind = 5
+        pad = torch.full((behind, C), 7.0, dtype=dt)
+        xx, dd = torch.cat([x, pad]).cuda(), torch.cat([dy, pad]).cuda()
+        mark = torch.full_like(xx, 3.0)
+        out = ccq.ccq_conv_fwd_varlen(xx, d(w), d(cu), max(lens), want_state=True,
+                                      out=dict(y=mark.clone()), **kw)
+        got = ccq.ccq_conv_bwd_varlen(xx, d(w), dd, d(cu), max(lens), dstateT=d(dsT),
+                                      out=dict(dx=mark.clone()), **kw)
+        for t in (out["y"], got["dx"]):
+            assert bool((t[len(x):] == 3.0).all())
+        out["y"], got["dx"] = out["y"][:len(x)], got["dx"][:len(x)]
+    else:
+        shp = (len(lens), lens[0], C)
+        out = ccq.ccq_conv_fwd(d(x).view(shp), d(w), want_state=True, **kw)
+        got = ccq.ccq_conv_bwd(d(x).view(shp), d(w), d(dy).view(shp), dstateT=d(dsT), **kw)
+        out["y"], got["dx"] = out["y"].view(-1, C), got["dx"].view(-1, C)
+    torch.cuda.synchronize()
+    close(out["y"], y.detach(), mag.detach(), dt, "y")
+    assert torch.equal(out["stateT"].cpu().double(), end.detach())
+    wmag = w.abs().sum(1).double() * 4 * dy.double().abs().max() + 1
+    close(got["dx"], ref["dx"], wmag.expand(len(x), C), dt, "dx")
+    if state:
+        close(got["dstate0"], ref["dstate0"], wmag.expand(len(lens), W - 1, C), dt, "dstate0")
+    # |dz| <= 1.1 |dy| + what the fast activation adds; the window's inputs against it
+    rows = torch.cat([x.new_zeros(W - 1, C) if s0 is None else s0.reshape(-1, C), x]).double().abs()
+    big = rows.amax(0) * dy.double().abs().sum(0) * 1.1 + 1
+    assert bool(((got["dw"].cpu().double() - ref["dw"]).abs() <= 2.0 ** -17 * big[:, None]).all())
+    if bias:
+        off = (got["dbias"].cpu().double() - ref["dbias"]).abs()
+        assert bool((off <= 2.0 ** -17 * (dy.double().abs().sum(0) * 1.1 + 1)).all())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_steps_continue_the_forward(dt):
+    """A prefix through the forward, the rest token by token on its state: the same bits."""
+    x, w, b, _, _, _ = make([40, 40, 40], 96, 4, dt, True, False)
+    x, w, b = x.cuda().view(3, 40, 96), w.cuda(), b.cuda()
+    whole = ccq.ccq_conv_fwd(x, w, bias=b, want_state=True)
+    for n in (0, 1, 2, 37):
+        head = ccq.ccq_conv_fwd(x[:, :n].contiguous(), w, bias=b, want_state=True)
+        assert torch.equal(head["y"], whole["y"][:, :n])
+        st = head["stateT"]
+        for t in range(n, 40):
+            y = ccq.ccq_conv_step(x[:, t].contiguous(), w, st, bias=b)
+            assert torch.equal(y, whole["y"][:, t])
+        assert torch.equal(st, whole["stateT"])
+
+
+def test_a_slice_of_a_projection_is_read_where_it_lies():
+    x, w, b, s0, dy, _ = make([50, 50], 64, 4, BF, True, True)
+    wide = torch.randn(2, 50, 64 + 40, device="cuda").to(BF)
+    wide[..., 24:88] = x.cuda().view(2, 50, 64)
+    part = wide[..., 24:88]
+    args = dict(bias=b.cuda(), state0=s0.cuda())
+    dense = part.contiguous()
+    assert torch.equal(ccq.ccq_conv_fwd(part, w.cuda(), **args)["y"],
+                       ccq.ccq_conv_fwd(dense, w.cuda(), **args)["y"])
+    dyc = dy.cuda().view(2, 50, 64)
+    a, b2 = (ccq.ccq_conv_bwd(t, w.cuda(), dyc, **args) for t in (part, dense))
+    assert all(torch.equal(a[n], b2[n]) for n in a)
+    st = s0.cuda().clone()
+    assert torch.equal(ccq.ccq_conv_step(part[:, 7], w.cuda(), st),
+                       ccq.ccq_conv_step(dense[:, 7].contiguous(), w.cuda(), s0.cuda().clone()))
+
+
+def test_gradient_against_differences():
+    """Central differences of sum(dy y) along random directions, fp32 io: the differences of two
+    fp32 sums over 2^-6 steps hold about 2^-24 2^6 of the sum of |dy y| (2^-13 with its terms)."""
+    x, w, b, s0, dy, _ = make([20], 16, 3, F32, True, True)
+    x, w, b, s0, dy = x.cuda().view(1, 20, 16), w.cuda(), b.cuda(), s0.cuda(), dy.cuda().view(1, 20, 16)
+    got = ccq.ccq_conv_bwd(x, w, dy, bias=b, state0=s0)
+
+    def loss(x, w, b, s0):
+        y = ccq.ccq_conv_fwd(x, w, bias=b, state0=s0)["y"]
+        return float((y.double() * dy.double()).sum())
+    args, h = [x, w, b, s0], 2.0 ** -6
+    for i, n in enumerate(("dx", "dw", "dbias", "dstate0")):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        v = torch.randn(args[i].shape, generator=g, device="cuda")
+        up, dn = list(args), list(args)
+        up[i], dn[i] = args[i] + h * v, args[i] - h * v
+        num = (loss(*up) - loss(*dn)) / (2 * h)
+        ana = float((got[n].double() * v.double()).sum())
+        # third derivatives of silu are below 1: h^2 / 6 of the cubed step, summed
+        size = float((dy.abs().sum()))
+        assert abs(num - ana) <= size * (2.0 ** -13 + h * h * 4), (n, num, ana)
+
+
+def test_out_may_not_share_memory():
+    x, w, b, s0, dy, _ = make([8], 64, 4, BF, True, True)
+    x, w = x.cuda().view(1, 8, 64), w.cuda()
+    with pytest.raises(ValueError):
+        ccq.ccq_conv_fwd(x, w, out=dict(y=x))
+    with pytest.raises(ValueError):
+        ccq.ccq_conv_fwd(x, w, out=dict(z=x))
+    with pytest.raises(ValueError):
+        ccq.ccq_conv_fwd(x.transpose(1, 2).contiguous().transpose(1, 2), w)  # channels apart
+    with pytest.raises(TypeError):
+        ccq.ccq_conv_fwd(x, w.to(BF))
+    with pytest.raises(ccq.CcqError):
+        ccq.ccq_conv_fwd(x, torch.zeros(64, 5, device="cuda"))
