@@ -23,17 +23,24 @@ namespace ccq {
 // form.  S_r and U are rounded to bf16 once, on store, for the kernels that form
 // outputs and gradients.
 //
-// What bounds the pass is the chain of chunks (B HV dv / 16 value tiles, a chunk
-// after the other), so one wave carries a value tile whole (16 columns of S^T,
-// all key features, in accumulators) and does nothing else; four more waves of
-// the workgroup stream the next chunk's operands into the other of two LDS slots
-// (global_load_lds, no registers).  One barrier a chunk.
-template <int DK, int NPR>
+// What bounds the pass is the chain of chunks (B HV dv / 16 value tiles of 16
+// columns of S^T, a chunk after the other).  NH waves carry a tile, each DK / NH of
+// its key features in accumulators, and do nothing else: splitting the features
+// shortens a chunk (its products and the splitting of S into heads and tails), at
+// the price of one exchange of the partial sums of K S^T through LDS.
+//
+// Four more waves of the workgroup stream the operands into LDS (global_load_lds,
+// no registers): two take the keys of every other chunk, two chunks ahead, into a
+// ring of three slots, two the transform, the values and the coefficients (X), one
+// chunk ahead, into two.  A loader has one chunk in flight at most, so it waits for
+// all of its loads and counts none.
+template <int DK, int NPR, int NH>
 struct DeltaTile {
-  static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NKH = DK / 32;
+  static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NC = NPR * NH;  // NC consumer waves
   static constexpr int KB = C * DK * 2, TB = C * C * 2, VB = C * BVS * 2, FB = 4 * C * 4;
-  static constexpr int SB = KB + 2 * TB + VB + FB, NSLOT = 2, LDS = NSLOT * SB;
-  static constexpr int NKL = KB / 1024 / NLW, NTL = TB / 1024 / NLW, NV = VB / 1024;  // 1 KB loads
+  static constexpr int XB = 2 * TB + VB + FB, SB = NH > 1 ? NC * 4 * 64 * 16 : 0;
+  static constexpr int KO = 0, XO = 3 * KB, SO = XO + 2 * XB, LDS = SO + SB;
+  static constexpr int NK = KB / 1024, NT = TB / 1024, NV = VB / 1024;  // 1 KB loads
 };
 
 template <int DK>
@@ -56,13 +63,15 @@ __device__ __forceinline__ void split_pair(const f32x4& x, const f32x4& y, Frag<
   }
 }
 
-template <int DK, int NPR>
-__global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_kernel(const GdnArgs a) {
+template <int DK, int NPR, int NH>
+__global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void delta_state_kernel(const GdnArgs a) {
   typedef bf16_t T;
   typedef __attribute__((address_space(3))) void lds_void;
-  typedef DeltaTile<DK, NPR> L;
-  constexpr int C = kChunk, BVS = L::BVS, NKH = L::NKH, NCT = DK / 16, RB = DK * 2;
-  static_assert(L::LDS <= 160 * 1024 && L::NKL >= 1 && L::KB / 1024 % L::NLW == 0, "LDS and load split");
+  typedef DeltaTile<DK, NPR, NH> L;
+  constexpr int C = kChunk, BVS = L::BVS, RB = DK * 2;
+  constexpr int DKH = DK / NH, NKH = DKH / 32, NCT = DKH / 16;  // a wave's features: blocks of 32, tiles
+  static_assert(NKH >= 1, "feature split");
+  static_assert(L::LDS <= 160 * 1024, "LDS");
   __shared__ __align__(1024) char smem[L::LDS];
 
   const int nvt = a.dv / BVS;
@@ -78,69 +87,107 @@ __global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int v0 = (lb % nvt) * BVS;
 
-  if (w >= NPR) {
+  if (w >= L::NC) {
     // ---- loaders: rows past the end of the sequence read the last row (finite
     // data; the chunk transform zeroes their contribution) ----
 #define CCQ_LDS(src, dst) __builtin_amdgcn_global_load_lds((const void*)(src), (lds_void*)(dst), 16, 0, 0)
-    const int lw = w - NPR;
-    const char* const kg = static_cast<const char*>(a.k);
-    const char* const vg = static_cast<const char*>(a.v);
+    const int lw = w - L::NC;
+    const bool keys = lw < 2;  // waves 0, 1: keys of chunks 0, 2, .. and 1, 3, ..; 2, 3: X
+    const int first = lw & 1;
+    constexpr int CPK = DK / 8, CPV = BVS / 8;  // 16-byte pieces per row
+    // A load covers R rows; its address is a uniform base and one of a few per-lane
+    // offsets formed once (the permutation repeats every 16 rows), so issuing it
+    // costs no vector arithmetic.  Rows past the end read the last row.
+    if (keys) {
+      constexpr int R = 64 / CPK, NP = 16 / R;
+      const char* const kg = static_cast<const char*>(a.k) + 2 * seq_off(sq, 0, kh.h, kh.H, DK);
+      const size_t pitch = (size_t)kh.H * RB;
+      uint32_t lane[NP];
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        lane[p] = (l / CPK) * (uint32_t)pitch + 16 * ((l % CPK) ^ dswz<DK>(p * R + l / CPK));
+      auto issue = [&](int ci) {
+        char* sb = smem + L::KO + (ci % 3) * L::KB;
+        const char* kc = kg + (size_t)ci * C * pitch;
+        const int nrow = sq.len - ci * C;
+        if (nrow >= C) {
+#pragma unroll
+          for (int i = 0; i < L::NK; ++i) CCQ_LDS(kc + i * R * pitch + lane[i % NP], sb + i * 1024);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < L::NK; ++i) {
+            const int row = i * R + l / CPK;
+            CCQ_LDS(kc + min(row, nrow - 1) * pitch + 16 * ((l % CPK) ^ dswz<DK>(row)), sb + i * 1024);
+          }
+        }
+      };
+      if (first < NLC) issue(first);
+#pragma unroll 1
+      for (int ci = 0; ci < NLC; ++ci) {
+        const bool mine = (ci & 1) == first;
+        if (mine) wait_vm_all();
+        __builtin_amdgcn_s_barrier();
+        if (mine && ci + 2 < NLC) issue(ci + 2);
+        if constexpr (NH > 1) __builtin_amdgcn_s_barrier();  // the consumers' exchange
+      }
+      return;
+    }
+    constexpr int R = 64 / CPV;
+    const char* const vg = static_cast<const char*>(a.v) + 2 * (seq_off(sq, 0, h, a.H, a.dv) + v0);
+    const size_t pitch = (size_t)a.H * a.dv * 2;
     const char* const tg = static_cast<const char*>(a.Tm) + (size_t)bh * N * L::TB;
     const char* const tl = static_cast<const char*>(a.TmLo) + (size_t)bh * N * L::TB;
     const float* const fg = a.gam + (size_t)bh * N * 5 * C;
-    constexpr int CPK = DK / 8, CPV = BVS / 8;  // 16-byte pieces per row
+    const uint32_t vlane = (l / CPV) * (uint32_t)pitch + 16 * (l % CPV);
+    const uint32_t tlane[2] = {(uint32_t)(16 * (l & ~7) + 16 * ((l % 8) ^ tswz(l / 8))),
+                               (uint32_t)(16 * (l & ~7) + 16 * ((l % 8) ^ tswz(8 + l / 8)))};
     auto issue = [&](int ci) {
-      char* sb = smem + (ci % L::NSLOT) * L::SB;
-      const int nrow = min(C, sq.len - ci * C);
-      const char* kc = kg + seq_off(sq, ci * C, kh.h, kh.H, DK) * 2;
-      const char* vc = vg + (seq_off(sq, ci * C, h, a.H, a.dv) + v0) * 2;
+      char* sb = smem + L::XO + (ci & 1) * L::XB;
+      const char* vc = vg + (size_t)ci * C * pitch;
+      const int nrow = sq.len - ci * C;
+      if (nrow >= C) {
 #pragma unroll
-      for (int it = 0; it < L::NKL; ++it) {
-        const int i = L::NLW * it + lw, row = i * (64 / CPK) + l / CPK;
-        CCQ_LDS(kc + (size_t)min(row, nrow - 1) * (kh.H * RB) + 16 * ((l % CPK) ^ dswz<DK>(row)), sb + i * 1024);
-      }
-#pragma unroll
-      for (int it = 0; it < L::NTL; ++it) {
-        const int i = L::NLW * it + lw, row = i * 8 + l / 8;
-        const size_t off = (size_t)ci * L::TB + row * (C * 2) + 16 * ((l % 8) ^ tswz(row));
-        CCQ_LDS(tg + off, sb + L::KB + i * 1024);
-        CCQ_LDS(tl + off, sb + L::KB + L::TB + i * 1024);
-      }
-#pragma unroll
-      for (int i = lw; i < L::NV; i += L::NLW) {
-        const int row = i * (64 / CPV) + l / CPV;
-        CCQ_LDS(vc + (size_t)min(row, nrow - 1) * (a.H * a.dv * 2) + 16 * (l % CPV), sb + L::KB + 2 * L::TB + i * 1024);
+        for (int i = 0; i < L::NV; ++i) CCQ_LDS(vc + i * R * pitch + vlane, sb + 2 * L::TB + i * 1024);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < L::NV; ++i)
+          CCQ_LDS(vc + min(i * R + l / CPV, nrow - 1) * pitch + 16 * (l % CPV), sb + 2 * L::TB + i * 1024);
       }
       // coefficient rows 1..4: beta e^gamma, beta, e^{gamma_C - gamma}, e^{gamma_C}
-      if (lw == L::NLW - 1) CCQ_LDS(fg + ((size_t)ci * 5 + 1) * C + 4 * l, sb + L::KB + 2 * L::TB + L::VB);
+      CCQ_LDS(fg + ((size_t)ci * 5 + 1) * C + 4 * l, sb + 2 * L::TB + L::VB);
+#pragma unroll
+      for (int i = 0; i < L::NT; ++i) {
+        CCQ_LDS(tg + (size_t)ci * L::TB + i * 1024 + tlane[i % 2], sb + i * 1024);
+        CCQ_LDS(tl + (size_t)ci * L::TB + i * 1024 + tlane[i % 2], sb + L::TB + i * 1024);
+      }
     };
-    if (NLC > 0) issue(0);
-    // At the barrier of chunk ci its slot has landed and the consumers are done
-    // with the other one, which chunk ci + 1 then takes: its loads have a whole
-    // chunk's time.
+    if (first == 0 && NLC > 0) issue(0);
 #pragma unroll 1
     for (int ci = 0; ci < NLC; ++ci) {
-      wait_vm_all();
+      const bool mine = (ci & 1) == first;
+      if (mine) wait_vm_all();
       __builtin_amdgcn_s_barrier();
-      if (ci + 1 < NLC) issue(ci + 1);
+      if (!mine && ci + 1 < NLC) issue(ci + 1);
+      if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
     }
     return;
 #undef CCQ_LDS
   }
 
-  // ---- consumer wave: value tile w of the workgroup's slice ----
-  const int v = v0 + 16 * w + c16;
-  // S^T[c][v] in pair order: c = pair_feat(tc, g4) + r
+  // ---- consumer wave: features c0 .. of value tile pr of the workgroup's slice ----
+  const int pr = w / NH, hq = w % NH, c0 = hq * DKH;
+  const int v = v0 + 16 * pr + c16;
+  // S^T[c][v] in pair order: c = c0 + pair_feat(tc, g4) + r
   f32x4 S[NCT];
 #pragma unroll
   for (int tc = 0; tc < NCT; ++tc) S[tc] = zero4();
   if (a.S0) {
-    const float* s0 = a.S0 + ((size_t)bh * a.dv + v) * DK + 8 * g4;
+    const float* s0 = a.S0 + ((size_t)bh * a.dv + v) * DK + c0 + 8 * g4;
 #pragma unroll
     for (int tc = 0; tc < NCT; ++tc) S[tc] = *reinterpret_cast<const f32x4*>(s0 + pair_feat(tc, 0));
   }
-  const int vt = (v0 >> 4) + w;
-  T* st_base = static_cast<T*>(a.states) + ((size_t)vt * NKH * 16 + c16) * 32 + 8 * g4;
+  const int vt = (v0 >> 4) + pr;
+  T* st_base = static_cast<T*>(a.states) + (((size_t)vt * (DK / 32) + hq * NKH) * 16 + c16) * 32 + 8 * g4;
   T* u_base = static_cast<T*>(a.U) + ((size_t)vt * 2 * 16 + c16) * 32 + 8 * g4;
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
   auto ldf = [](const char* p) {
@@ -150,35 +197,38 @@ __global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_
   };
   auto tr = [](const char* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p); };
   // The permutation of K touches the low bits of the piece index only (four, or
-  // three at dk = 64), so a lane's block m of 32 features lies 256 (m / 4) bytes
-  // on from block m % 4.  krow: row c16, piece 4 m + g4 (row operands); kcol:
-  // transposing reads, rows 4 g4 + j / 4 (j = c16), piece 4 m + j % 4 (+ 8 bytes
-  // for odd tiles)
+  // three at dk = 64), so block m of 32 features (counted from the wave's first, M
+  // = c0 / 32 + m) lies 256 (M / 4) bytes on from block M % 4.  krow: row c16, piece
+  // 4 M + g4 (row operands); kcol: transposing reads, rows 4 g4 + j / 4 (j = c16),
+  // piece 4 M + j % 4 (+ 8 bytes for odd tiles)
   constexpr int NQ = NKH < 4 ? NKH : 4;
   int krow[NQ], kcol[NQ];
   {
     const int rr = 4 * g4 + (c16 >> 2);
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      krow[q] = c16 * RB + 16 * ((4 * q + g4) ^ dswz<DK>(c16));
-      kcol[q] = rr * RB + 16 * ((4 * q + (c16 & 3)) ^ dswz<DK>(rr));
+      const int M = c0 / 32 + q;  // (NKH < 4: the wave's blocks lie within one group of four)
+      krow[q] = c16 * RB + (M >> 2) * 256 + 16 * ((4 * (M & 3) + g4) ^ dswz<DK>(c16));
+      kcol[q] = rr * RB + (M >> 2) * 256 + 16 * ((4 * (M & 3) + (c16 & 3)) ^ dswz<DK>(rr));
     }
   }
   const int trow = c16 * (C * 2) + 16 * (g4 ^ tswz(c16));  // Tm row c16, columns 8 g4 ..; 32 on: ^ 64
-  const int vrow = (4 * g4 + (c16 >> 2)) * (2 * BVS) + 32 * w + 8 * (c16 & 3);
+  const int vrow = (4 * g4 + (c16 >> 2)) * (2 * BVS) + 32 * pr + 8 * (c16 & 3);
+  f32x4* const sX = reinterpret_cast<f32x4*>(smem + L::SO);
 
+  // S as operands: head and tail, renewed tile by tile behind the update's products
+  Frag<T> sh[NKH], sl[NKH];
+#pragma unroll
+  for (int m = 0; m < NKH; ++m) split_pair(S[2 * m], S[2 * m + 1], sh[m], sl[m]);
   int until = 0;  // chunks until the next stored state
 #pragma unroll 1
   for (int ci = 0; ci < NLC; ++ci) {
-    const char* kb = smem + (ci % L::NSLOT) * L::SB;
-    const char* th = kb + L::KB;
+    const char* kb = smem + L::KO + (ci % 3) * L::KB;
+    const char* th = smem + L::XO + (ci & 1) * L::XB;
     const char* tl = th + L::TB;
     const char* vb = tl + L::TB;
     const float* Fb = reinterpret_cast<const float*>(vb + L::VB);
-    Frag<T> sh[NKH], sl[NKH];
-#pragma unroll
-    for (int m = 0; m < NKH; ++m) split_pair(S[2 * m], S[2 * m + 1], sh[m], sl[m]);
-    lds_barrier();  // this chunk's slot has landed, the other one is free
+    lds_barrier();  // this chunk's operands have landed, the slots of the one before are free
     // R = beta V - beta e^gamma K S_r^T, token tile J in accumulators.  LDS reads
     // run one group of GB feature blocks ahead of their products (the scheduling
     // barriers keep the compiler from sinking them): the wave is alone on its
@@ -191,52 +241,84 @@ __global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_
       for (int m = 0; m < GB; ++m)
         kf[step & 1][m] = ldf(kb + krow[(m0 + m) & 3] + ((m0 + m) >> 2) * 256 + 16 * J * RB);
     };
-    const float eC = Fb[3 * C];
     read_k(0);
-    f32x4 R[4];
+    f32x4 R[4], bv[4], bg[4];
     Frag<T> tmh[4][2], tml[4][2];
+    // Tm (rows stored in acc_pos order; the second half of rows 0..31 is zero),
+    // beta V and beta e^gamma, requested among the products
+    auto read_tm = [&](int I) {
+      tmh[I][0] = ldf(th + trow + 16 * I * (C * 2));
+      tml[I][0] = ldf(tl + trow + 16 * I * (C * 2));
+      if (I >= 2) {
+        tmh[I][1] = ldf(th + (trow ^ 64) + 16 * I * (C * 2));
+        tml[I][1] = ldf(tl + (trow ^ 64) + 16 * I * (C * 2));
+      }
+    };
+    auto read_v = [&](int J) {
+      const bf16x4 vv = tr(vb + vrow + 16 * J * 2 * BVS);
+      const f32x4 bj = *reinterpret_cast<const f32x4*>(Fb + C + 16 * J + 4 * g4);
+      bg[J] = *reinterpret_cast<const f32x4*>(Fb + 16 * J + 4 * g4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) bv[J][r] = bj[r] * f32(vv[r]);
+    };
+    const float eC = Fb[3 * C];
+    f32x4 x[4][2];
+    // a tile's sums, one tile behind its products: the partial ones to the exchange,
+    // or (one wave a value tile) R itself
+    auto finish = [&](int J) {
+      R[J] = x[J][0] + x[J][1];
+      if constexpr (NH > 1) {
+        sX[(w * 4 + J) * 64 + l] = R[J];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) R[J][r] = bv[J][r] - bg[J][r] * R[J][r];
+      }
+    };
 #pragma unroll
     for (int J = 0; J < 4; ++J) {
-      const bf16x4 vv = tr(vb + vrow + 16 * J * 2 * BVS);
-      const f32x4 bg = *reinterpret_cast<const f32x4*>(Fb + 16 * J + 4 * g4);
-      const f32x4 bj = *reinterpret_cast<const f32x4*>(Fb + C + 16 * J + 4 * g4);
-      f32x4 x[4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) x[g] = zero4();
+      x[J][0] = zero4();
+      x[J][1] = zero4();
 #pragma unroll
       for (int gb = 0; gb < NGB; ++gb) {
         const int step = J * NGB + gb;
-        if (step + 1 < 4 * NGB) {
-          read_k(step + 1);
-        } else {  // Tm (rows stored in acc_pos order; the second half of rows 0..31 is zero)
-#pragma unroll
-          for (int I = 0; I < 4; ++I) {
-            tmh[I][0] = ldf(th + trow + 16 * I * (C * 2));
-            tml[I][0] = ldf(tl + trow + 16 * I * (C * 2));
-            if (I >= 2) {
-              tmh[I][1] = ldf(th + (trow ^ 64) + 16 * I * (C * 2));
-              tml[I][1] = ldf(tl + (trow ^ 64) + 16 * I * (C * 2));
-            }
-          }
+        if (step + 1 < 4 * NGB) read_k(step + 1);
+        if (gb == NGB - 1) {
+          read_v(J);
+          if (NH > 1 && J > 0) read_tm(J - 1);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < GB; ++m) {
-          mma(x[m & 1], kf[step & 1][m], sh[gb * GB + m]);
-          mma(x[2 + (m & 1)], kf[step & 1][m], sl[gb * GB + m]);
+          mma(x[J][0], kf[step & 1][m], sh[gb * GB + m]);
+          mma(x[J][1], kf[step & 1][m], sl[gb * GB + m]);
         }
       }
 #pragma unroll
-      for (int t = 0; t < NCT / 4; ++t) S[NCT / 4 * J + t] *= eC;
-      const f32x4 sum = (x[0] + x[1]) + (x[2] + x[3]);
+      for (int t = J * NCT / 4; t < (J + 1) * NCT / 4; ++t) S[t] *= eC;
+      if (J > 0) finish(J - 1);
+    }
+    finish(3);
+    if constexpr (NH > 1) {
+      read_tm(3);
+      lds_barrier();
+      // the tile's partial sums in a fixed order: its waves hold the same bits
 #pragma unroll
-      for (int r = 0; r < 4; ++r) R[J][r] = bj[r] * f32(vv[r]) - bg[r] * sum[r];
+      for (int J = 0; J < 4; ++J) {
+        f32x4 sum = sX[(pr * NH * 4 + J) * 64 + l];
+#pragma unroll
+        for (int hh = 1; hh < NH; ++hh) sum += sX[((pr * NH + hh) * 4 + J) * 64 + l];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) R[J][r] = bv[J][r] - bg[J][r] * sum[r];
+      }
+    } else {
+#pragma unroll
+      for (int I = 0; I < 4; ++I) read_tm(I);
     }
     Frag<T> rh[2], rl[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) split_pair(R[2 * q], R[2 * q + 1], rh[q], rl[q]);
     // K^T of TB feature tiles at a time, for the update
-    constexpr int TB = 4;
+    constexpr int TB = NCT < 4 ? NCT : 4;
     Frag<T> tf[2][TB][2];
     auto read_t = [&](int tc0, Frag<T>(&f)[TB][2]) {
 #pragma unroll
@@ -280,6 +362,19 @@ __global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_
       U[2 * q + 1] *= dd[2 * q + 1];
       split_pair(U[2 * q], U[2 * q + 1], uh[q], ul[q]);
     }
+    // S_r (every sstride-th chunk) and U^T, fragment-native
+    if (until == 0) {
+      T* st_out = st_base + ((size_t)bh * N + ci) * a.dv * DK;
+#pragma unroll
+      for (int m = 0; m < NKH; ++m) store_frag(st_out + 16 * 32 * m, sh[m]);
+      until = a.sstride;
+    }
+    --until;
+    if (hq == 0) {
+      T* u_out = u_base + ((size_t)bh * N + ci) * a.dv * C;
+      store_frag(u_out, uf[0]);
+      store_frag(u_out + 16 * 32, uf[1]);
+    }
     // S^T <- e^{gamma_C} S^T + K^T diag(e^{gamma_C - gamma}) U
 #pragma unroll
     for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {
@@ -292,22 +387,16 @@ __global__ __launch_bounds__(64 * (NPR + 4 < 8 ? 8 : NPR + 4)) void delta_state_
 #pragma unroll
         for (int t = 0; t < TB; ++t) mma(S[TB * tb4 + t], tf[tb4 & 1][t][kq], uh[kq]);
       }
-    }
-    // S_r (every sstride-th chunk) and U^T, fragment-native
-    if (until == 0) {
-      T* st_out = st_base + ((size_t)bh * N + ci) * a.dv * DK;
+      if (tb4 > 0)
 #pragma unroll
-      for (int m = 0; m < NKH; ++m) store_frag(st_out + 16 * 32 * m, sh[m]);
-      until = a.sstride;
+        for (int m = TB / 2 * (tb4 - 1); m < TB / 2 * tb4; ++m) split_pair(S[2 * m], S[2 * m + 1], sh[m], sl[m]);
     }
-    --until;
-    T* u_out = u_base + ((size_t)bh * N + ci) * a.dv * C;
-    store_frag(u_out, uf[0]);
-    store_frag(u_out + 16 * 32, uf[1]);
+#pragma unroll
+    for (int m = NKH - TB / 2; m < NKH; ++m) split_pair(S[2 * m], S[2 * m + 1], sh[m], sl[m]);
   }
 
   if (a.ST) {
-    float* st = a.ST + ((size_t)bh * a.dv + v) * DK + 8 * g4;
+    float* st = a.ST + ((size_t)bh * a.dv + v) * DK + c0 + 8 * g4;
 #pragma unroll
     for (int tc = 0; tc < NCT; ++tc) *reinterpret_cast<f32x4*>(st + pair_feat(tc, 0)) = S[tc];
   }
@@ -395,21 +484,37 @@ __global__ __launch_bounds__(256) void head_sum_kernel(const HeadSumArgs a) {
 }
 
 namespace {
-template <int DK, int NPR>
+template <int DK, int NPR, int NH>
 hipError_t run_delta_state(const GdnArgs& a, hipStream_t st) {
+  typedef DeltaTile<DK, NPR, NH> L;
   const int nblk = a.B * a.H * (a.dv / (16 * NPR));
   if (nblk == 0) return hipSuccess;
-  hipLaunchKernelGGL((delta_state_kernel<DK, NPR>), dim3(nblk), dim3(64 * (NPR + DeltaTile<DK, NPR>::NLW)), 0, st, a);
+  hipLaunchKernelGGL((delta_state_kernel<DK, NPR, NH>), dim3(nblk), dim3(64 * (L::NC + L::NLW)), 0, st, a);
   return hipGetLastError();
 }
-// One value tile per workgroup while every tile can have a compute unit of its
-// own, else two, else four (where a workgroup's LDS admits them).
+// Value tiles a workgroup and waves a tile, by the number of tiles (state pass
+// alone, 32 chunks): a compute unit to every tile while there are enough, the
+// features then split where that pays; from there on more tiles a workgroup, so
+// that all of them run at once.
+//   dk = 256:  128 tiles  69 us at 1 x 4 waves, 83 at 2 x 2;   512: 84 at 2 x 2, 133 at 1 x 4;
+//             1024        153 at 2 x 2, 249 at 1 x 4
+//   dk = 128:  128        57 at 1 x 4, 61 at 2 x 1, 63 at 4 x 1;  512: 63 at 2 x 1, 66 at 2 x 2;
+//             1024        70 at 4 x 1, 116 at 2 x 1, 190 at 8 x 1
+//   dk = 64:    64        42 at 2 x 1, 45 at 1 x 2;  512: 44 at 2 x 1, 48 at 4 x 1;
+//             2048        49 at 8 x 1, 59 at 4 x 1, 93 at 2 x 1
 template <int DK>
 hipError_t run_delta_state_dk(const GdnArgs& a, hipStream_t st) {
   const long long tiles = (long long)a.B * a.H * (a.dv / 16);
-  if (tiles <= 256) return run_delta_state<DK, 1>(a, st);
-  if (tiles <= 512) return run_delta_state<DK, 2>(a, st);
-  return run_delta_state<DK, 4>(a, st);
+  if constexpr (DK == 64) {
+    if (tiles > 1024 && a.dv % 128 == 0) return run_delta_state<DK, 8, 1>(a, st);
+    if (tiles > 512) return run_delta_state<DK, 4, 1>(a, st);
+    return run_delta_state<DK, 2, 1>(a, st);
+  } else {
+    if (tiles <= 256) return run_delta_state<DK, 1, 4>(a, st);
+    if constexpr (DK == 256) return run_delta_state<DK, 2, 2>(a, st);
+    else if (tiles > 512) return run_delta_state<DK, 4, 1>(a, st);
+    else return run_delta_state<DK, 2, 1>(a, st);
+  }
 }
 template <typename T>
 hipError_t step_dispatch(const DeltaStepArgs& a, hipStream_t st) {
