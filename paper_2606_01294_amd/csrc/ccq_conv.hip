@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_bias(float (&b)[VE], const float* p, int c)
 }
 }  // namespace
 
-template <typename T, int W, int VE>
+template <typename T, int W, int VE, int ACT>
 __global__ __launch_bounds__(kConvThreads) void conv_fwd_kernel(const ConvArgs a) {
   typedef VecN<T, VE> V;
   constexpr int NB = 8;  // rows requested together
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_fwd_kernel(const ConvArgs a
         float z = bias[e];
 #pragma unroll
         for (int j = 0; j < W; ++j) z += w[j][e] * win[j][e];
-        o[e] = Act<T>::value(a.act, z);
+        o[e] = Act<T>::value(ACT, z);
       }
       if (tb + i < t1) V::store(y + (size_t)(tb + i) * a.C, o);
     }
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(const ConvArgs 
 // Workgroup: 64 channel vectors x 4 consecutive runs (a wave each) of one
 // sequence.  Its sums go to partial row blockIdx.x / column blocks: W planes of
 // C columns for dw, one for db.
-template <typename T, int W, int VE>
+template <typename T, int W, int VE, int ACT>
 __global__ __launch_bounds__(kConvThreads) void conv_bwd_kernel(const ConvArgs a) {
   typedef VecN<T, VE> V;
   constexpr int NB = 4;
@@ -162,7 +162,8 @@ __global__ __launch_bounds__(kConvThreads) void conv_bwd_kernel(const ConvArgs a
   const unsigned rb = blockIdx.x / ncb;  // partial row: sequence and group of four runs
   const int cb = blockIdx.x - rb * ncb;
   const int groups = (a.runs + 3) / 4;
-  const int b = rb / groups, run = 4 * (int)(rb - b * groups) + wave_id();
+  // (a wave's run is uniform: its bounds and branches are scalar)
+  const int b = rb / groups, run = 4 * (int)(rb - b * groups) + __builtin_amdgcn_readfirstlane(wave_id());
   const int cv = cb * 64 + lane_id();
   const bool mine = cv < CV;
   const int c = mine ? cv * VE : 0;
@@ -205,15 +206,25 @@ __global__ __launch_bounds__(kConvThreads) void conv_bwd_kernel(const ConvArgs a
     }
     // tokens t0 .. t1 + W - 2: the last W - 1 only complete the dx before them
     const int te = t1 + W - 1;
-    for (int tb = t0; tb < te; tb += NB) {
-      typename V::raw rx[NB], rd[NB];
-      if (tb < sq.len)
+    typename V::raw nx[NB], nd[NB];  // the rows of the next batch, requested a batch ahead
+    auto request = [&](int tb) {
+      if (tb < sq.len && tb < te)
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           const int t = min(tb + i, sq.len - 1);
-          rx[i] = V::load(x + (size_t)t * a.ldx);
-          rd[i] = V::load(dy + (size_t)t * a.C);
+          nx[i] = V::load(x + (size_t)t * a.ldx);
+          nd[i] = V::load(dy + (size_t)t * a.C);
         }
+    };
+    request(t0);
+    for (int tb = t0; tb < te; tb += NB) {
+      typename V::raw rx[NB], rd[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        rx[i] = nx[i];
+        rd[i] = nd[i];
+      }
+      request(tb + NB);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const int t = tb + i;
@@ -232,7 +243,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_bwd_kernel(const ConvArgs a
             float z = bias[e], v, d;
 #pragma unroll
             for (int j = 0; j < W; ++j) z += w[j][e] * win[j][e];
-            Act<T>::both(a.act, z, v, d);
+            Act<T>::both(ACT, z, v, d);
             dz[W - 1][e] = V::get(rd[i], e) * d;
           }
           if (t < t1)
@@ -294,13 +305,15 @@ constexpr int kConvVeB = 4;
 
 int conv_runs(int T, int len) { return T > 0 ? (T + len - 1) / len : 1; }
 
-template <typename T, int W>
+// The activation is a constant of the kernels: a branch on it at every element cost
+// the backward 44 instead of 38 us at 12,100 packed tokens of 2048 channels.
+template <typename T, int W, int ACT>
 hipError_t run_conv(ConvArgs a, ConvCall call, hipStream_t st) {
   if (call == ConvCall::kBwd) {
     a.runs = conv_runs(a.T, kConvRunB);
     const long long ncb = (a.C / kConvVeB + 63) / 64;
     const long long nblk = conv_part_rows(a.B, a.T) * ncb;
-    hipLaunchKernelGGL((conv_bwd_kernel<T, W, kConvVeB>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
+    hipLaunchKernelGGL((conv_bwd_kernel<T, W, kConvVeB, ACT>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
     return hipGetLastError();
   }
   constexpr int VE = conv_ve<T>();
@@ -312,15 +325,24 @@ hipError_t run_conv(ConvArgs a, ConvCall call, hipStream_t st) {
   }
   a.runs = conv_runs(a.T, kConvRun);
   const long long nblk = ((long long)a.B * a.runs * cv + kConvThreads - 1) / kConvThreads;
-  hipLaunchKernelGGL((conv_fwd_kernel<T, W, VE>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
+  hipLaunchKernelGGL((conv_fwd_kernel<T, W, VE, ACT>), dim3((unsigned)nblk), dim3(kConvThreads), 0, st, a);
   return hipGetLastError();
+}
+template <typename T, int W>
+hipError_t conv_act(const ConvArgs& a, ConvCall call, hipStream_t st) {
+  switch (a.act) {
+    case kActNone: return run_conv<T, W, kActNone>(a, call, st);
+    case kActSilu: return run_conv<T, W, kActSilu>(a, call, st);
+    case kActSigmoid: return run_conv<T, W, kActSigmoid>(a, call, st);
+  }
+  return hipErrorInvalidValue;
 }
 template <typename T>
 hipError_t conv_dispatch(const ConvArgs& a, int W, ConvCall call, hipStream_t st) {
   switch (W) {
-    case 2: return run_conv<T, 2>(a, call, st);
-    case 3: return run_conv<T, 3>(a, call, st);
-    case 4: return run_conv<T, 4>(a, call, st);
+    case 2: return conv_act<T, 2>(a, call, st);
+    case 3: return conv_act<T, 3>(a, call, st);
+    case 4: return conv_act<T, 4>(a, call, st);
   }
   return hipErrorInvalidValue;
 }
@@ -339,25 +361,32 @@ hipError_t launch_conv(const ConvArgs& a, int W, ConvCall call, bool is_bf16, hi
 }
 
 // ----------------------------------------------------------------------------
-// Column sums of a [rows, cols] matrix of partial sums, in a fixed order: 32
-// columns per workgroup, 32 threads sharing a column's rows.
+// Column sums of a [rows, cols] matrix of partial sums, in a fixed order: 16
+// columns per workgroup, 64 threads sharing a column's rows, eight loads in flight
+// each (few rows and columns: latency is all there is).
 namespace {
-constexpr int kSumCols = 32, kSumRows = 32;
+constexpr int kSumCols = 16, kSumRows = 64;
 }
 __global__ __launch_bounds__(kSumCols * kSumRows) void colsum_kernel(const ColsumArgs a) {
   __shared__ float buf[kSumRows][kSumCols + 1];
   const int cl = threadIdx.x % kSumCols, rl = threadIdx.x / kSumCols;
   const int col = blockIdx.x * kSumCols + cl;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  float s[U] = {};
   if (col < a.cols) {
     const float* p = a.part + col;
-    long long r = rl;
-    for (; r + 3 * kSumRows < a.rows; r += 4 * kSumRows)
+    for (long long r = rl; r < a.rows; r += U * kSumRows) {
+      float x[U];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += p[(size_t)(r + q * kSumRows) * a.cols];
-    for (; r < a.rows; r += kSumRows) s[0] += p[(size_t)r * a.cols];
+      for (int q = 0; q < U; ++q) {
+        const long long rq = r + q * kSumRows;
+        x[q] = p[(size_t)(rq < a.rows ? rq : r) * a.cols];
+      }
+#pragma unroll
+      for (int q = 0; q < U; ++q) s[q] += r + q * kSumRows < a.rows ? x[q] : 0.f;
+    }
   }
-  buf[rl][cl] = (s[0] + s[1]) + (s[2] + s[3]);
+  buf[rl][cl] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
   __syncthreads();
   if (rl == 0 && col < a.cols) {
     float t = 0.f;

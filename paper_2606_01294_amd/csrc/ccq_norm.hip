@@ -14,11 +14,12 @@
 // Both directions read every tensor once and keep an item in registers between
 // its sums and its use, so HBM bounds them.  An item is held by LPI consecutive
 // lanes (a power of two, up to a wave; a workgroup above 1024 channels), NV vectors
-// of eight channels each.  A slot of LPI lanes takes the items s, s + NS, ... with
-// NS a multiple of G: its head never changes, so the weights are read once and the
-// backward sums dw and db in registers, over all of a slot's rows.  The sums of the
-// slots (of the workgroups, where the heads share one weight) meet in a second
-// kernel in a fixed order: no atomics, the same bits every time.
+// of eight channels each.  A slot of LPI lanes takes one head of the rows r, r +
+// step, ..: its weights are read once, and the backward sums dw and db in registers
+// over all of its rows.  Forward, consecutive slots take consecutive heads (whole
+// rows are read); backward, a workgroup's slots take the same head of different rows,
+// so that its sums meet in LDS and it leaves one row of partial sums, which a second
+// kernel adds up in a fixed order: no atomics, the same bits every time.
 // Sums, statistics and the affine part are fp32; what is stored is rounded once.
 #include "ccq_device.h"
 #include "ccq_kernels.h"
@@ -150,17 +151,19 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_kernel(const NormArgs a
   }
 }
 
-// dw and db of a slot's rows go to partial row s / G, columns head D + .. (or,
-// with one weight for all heads, the workgroup's sum to row blockIdx.x), db
-// behind all of dw.
+// Workgroup: head blockIdx.x % G, its slots the rows r, r + 1, .. of row block
+// blockIdx.x / G.  Its sums go to partial row blockIdx.x / G, columns head D + ..
+// (with one weight for all heads: to a row of their own, columns 0 ..), db behind
+// all of dw.
 template <typename T, int LPI, int NV, bool GATE>
 __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a) {
   typedef Vec8<T> V;
   constexpr int SPW = LPI < 64 ? 64 / LPI : 1;  // slots per wave
+  constexpr int SPB = kNormThreads / LPI;       // per workgroup
   __shared__ float red[4];
-  const long long s = ((long long)blockIdx.x * kNormThreads + threadIdx.x) / LPI;
   const ItemCols<LPI, NV> ic{(int)(threadIdx.x % LPI), a.D / 8};
-  const int head = (int)(s % a.G);
+  const unsigned rb = blockIdx.x / a.G;
+  const int head = blockIdx.x - rb * a.G;
   const long long step = a.slots / a.G;
   const T* x = static_cast<const T*>(a.x) + (size_t)head * a.D;
   const T* gate = static_cast<const T*>(a.gate) + (size_t)head * a.D;
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a
         rd[u] = V::load(dy + (size_t)row * ldy + ic.col(u));
       }
   };
-  const long long first = s < a.slots ? s / a.G : a.rows;  // (slots behind the last one: no rows)
+  const long long first = (long long)rb * SPB + threadIdx.x / LPI;
   if (first < a.rows) load(first);
   for (long long row = first; row < a.rows; row += step) {
     float n[NV][8], g[NV][8], d[NV][8];
@@ -244,22 +247,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a
   const bool bias = a.bias != nullptr;
   const size_t cols = (size_t)(a.shared ? 1 : a.G) * a.D;  // of dw
   const size_t pitch = cols * (bias ? 2 : 1);
-  if (!a.shared) {
-    if (s >= a.slots) return;
-    float* out = a.part + (size_t)(s / a.G) * pitch + (size_t)head * a.D;
-#pragma unroll
-    for (int u = 0; u < NV; ++u)
-      if (ic.has(u))
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          out[ic.col(u) + e] = dw[u][e];
-          if (bias) out[cols + ic.col(u) + e] = db[u][e];
-        }
-    return;
-  }
-  // one weight for all heads: the workgroup's slots are summed first
   __shared__ float buf[LPI > 64 ? 1 : 4][LPI > 64 ? 1 : LPI * NV * 8];
-  float* out = a.part + (size_t)blockIdx.x * pitch;
+  float* out = a.part + (a.shared ? (size_t)blockIdx.x * pitch : (size_t)rb * pitch + (size_t)head * a.D);
   for (int q = 0; q < (bias ? 2 : 1); ++q) {
 #pragma unroll
     for (int u = 0; u < NV; ++u)
@@ -292,21 +281,24 @@ int norm_lanes(int D) {  // lanes that hold an item: 8 channels each, a power of
   return nvec > 128 ? 256 : l;
 }
 
-// Slots: enough waves to fill the chip and no more, so that a slot's weights (and
-// in the backward its sums) serve many rows; always a multiple of G.  Forward: 32
-// waves a compute unit; backward: 16.
-long long norm_slots(long long rows, int G, int lanes, bool bwd) {
-  const long long threads = 256ll * (bwd ? 16 : 32) * 64;
-  long long step = (threads / lanes + G - 1) / G;
+// Slots, a multiple of G.  Forward: enough for 32 waves a compute unit and no more,
+// so that a slot's weights serve many rows.
+long long norm_slots(long long rows, int G, int lanes) {
+  long long step = (256ll * 32 * 64 / lanes + G - 1) / G;
   if (step < 1) step = 1;
   return (rows < step ? rows : step) * G;
 }
-
-long long norm_blocks(long long slots, int lanes) { return (slots * lanes + kNormThreads - 1) / kNormThreads; }
-
+// Backward: row blocks of SPB rows at a time for each head, 4 workgroups a compute
+// unit in all (what its registers admit).
+long long norm_row_blocks(long long rows, int G, int lanes) {
+  const long long spb = kNormThreads / lanes;
+  const long long most = (1024 + G - 1) / G, need = (rows + spb - 1) / spb;
+  return most < need ? most : need;
+}
 template <typename T, int LPI, int NV>
 hipError_t run_norm(const NormArgs& a, bool bwd, hipStream_t st) {
-  const dim3 grid((unsigned)norm_blocks(a.slots, LPI)), block(kNormThreads);
+  const long long nblk = bwd ? norm_row_blocks(a.rows, a.G, LPI) * a.G : (a.slots * LPI + kNormThreads - 1) / kNormThreads;
+  const dim3 grid((unsigned)nblk), block(kNormThreads);
   if (!bwd) {
     if (a.gate) hipLaunchKernelGGL((norm_fwd_kernel<T, LPI, NV, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((norm_fwd_kernel<T, LPI, NV, false>), grid, block, 0, st, a);
@@ -342,13 +334,12 @@ bool norm_supported(int D) { return D >= 8 && D <= 8192 && D % 8 == 0; }
 
 // Rows of partial sums of dw (and db) that the backward leaves for colsum.
 long long norm_part_rows(long long rows, int G, int D, int shared) {
-  const int lanes = norm_lanes(D);
-  const long long slots = norm_slots(rows, G, lanes, true);
-  return shared ? norm_blocks(slots, lanes) : slots / G;
+  return norm_row_blocks(rows, G, norm_lanes(D)) * (shared ? G : 1);
 }
 
 hipError_t launch_norm(NormArgs a, bool is_bf16, bool bwd, hipStream_t st) {
-  a.slots = norm_slots(a.rows, a.G, norm_lanes(a.D), bwd);
+  const int lanes = norm_lanes(a.D);
+  a.slots = bwd ? norm_row_blocks(a.rows, a.G, lanes) * (kNormThreads / lanes) * a.G : norm_slots(a.rows, a.G, lanes);
   return is_bf16 ? norm_dispatch<bf16_t>(a, bwd, st) : norm_dispatch<float>(a, bwd, st);
 }
 

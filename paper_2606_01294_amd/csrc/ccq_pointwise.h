@@ -23,14 +23,24 @@ struct VecN {
 template <typename T> using Vec8 = VecN<T, 8>;
 
 // act(z) and act'(z): none, silu (z sigmoid z), sigmoid.  bf16 io takes the
-// hardware's exponential and reciprocal (about 1e-6 relative, far below the
-// 2^-9 of the rounding on store); fp32 io the full-precision ones.  exp(-z)
-// overflows to infinity for z < -88, where sigmoid is then an exact 0.
+// hardware's exponential and reciprocal as they are (about 1e-6 relative, far
+// below the 2^-9 of the rounding on store).  fp32 io adds what they lack: the
+// rounding of z log2(e), which e^r = 1 + r takes back, and one Newton step of the
+// reciprocal (a few 2^-24 in all, in ten instructions).  exp(-z) overflows to
+// infinity for z < -88, where sigmoid is then an exact 0.
 template <typename T>
 struct Act {
   static __device__ __forceinline__ float sigmoid(float z) {
     if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
-    else return 1.f / (1.f + expf(-z));
+    const float t = -z * 1.44269504f;
+    // -z log2(e) - t, with log2(e) to 48 bits
+    float r = __builtin_fmaf(-z, 1.44269504f, -t);
+    r = __builtin_fmaf(-z, 1.92596303e-8f, r);
+    r = fabsf(t) < 1e30f ? r * 0.693147181f : 0.f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    const float d = 1.f + __builtin_fmaf(e, r, e);
+    const float q = __builtin_amdgcn_rcpf(d);
+    return d < 3e38f ? __builtin_fmaf(__builtin_fmaf(-d, q, 1.f), q, q) : q;
   }
   static __device__ __forceinline__ float value(int act, float z) {
     if (act == kActNone) return z;
