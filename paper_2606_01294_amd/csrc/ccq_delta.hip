@@ -4,6 +4,8 @@
 // The chunked form is that of ccq_gdn.hip (transforms Tm, state pass, outputs),
 // read with the caller's queries; value head h reads query/key head h / (HV / HK).
 // Its backward is that of ccq_gdn_bwd.hip.
+#include <type_traits>
+
 #include "ccq_device.h"
 #include "ccq_kernels.h"
 
@@ -403,6 +405,341 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 }
 
 // ----------------------------------------------------------------------------
+// Reverse scan of D = dL/dS_{r+1} (bf16 io), last chunk to first, with dO the
+// upstream gradient and s the read scale (see ccq_gdn_bwd.hip):
+//
+//   dU = diag(e^{gamma_C - gamma}) K D^T + s P^T dO,   dR = Tm^T dU   (stored),
+//   D <- e^{gamma_C} D + Q^T (s diag(e^gamma) dO) - K^T diag(beta e^gamma) dR.
+//
+// D (as it enters the chunk) and dR are stored for the chunk-parallel gradients.
+// Bound, as the state pass, by the chain of chunks and laid out like it: NH
+// consumer waves a value tile of 16 columns of D^T, the features of a tile split
+// over them (one exchange of the partial dU), four waves that only stream.  K and
+// X (P^T, Tm^T, dO, coefficients) come one chunk ahead into two slots each; Q, which
+// only the end of a chunk reads, into one: its loads go out when the chunk begins
+// and a barrier of its own stands before its products.  Operands are bf16, D and
+// every sum fp32 (D and dR are rounded as operands and on store).
+template <int DK, int NPR, int NH>
+struct DeltaBackTile {
+  static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NC = NPR * NH;
+  static constexpr int KB = C * DK * 2, TB = C * C * 2, VB = C * BVS * 2, FB = 5 * C * 4;
+  static constexpr int XB = 2 * TB + VB + FB, SB = NH > 1 ? NC * 4 * 64 * 16 : 0;
+  static constexpr int QO = 2 * KB, XO = QO + KB, SO = XO + 2 * XB, LDS = SO + SB;
+  static constexpr int NK = KB / 1024, NT = TB / 1024, NV = VB / 1024;  // 1 KB loads
+};
+
+template <int DK, int NPR, int NH>
+__global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void delta_dstate_kernel(const GdnDstateArgs a) {
+  typedef bf16_t T;
+  typedef __attribute__((address_space(3))) void lds_void;
+  typedef DeltaBackTile<DK, NPR, NH> L;
+  constexpr int C = kChunk, BVS = L::BVS, RB = DK * 2;
+  constexpr int DKH = DK / NH, NKH = DKH / 32, NCT = DKH / 16;
+  static_assert(NKH >= 1 && L::LDS <= 160 * 1024, "feature split, LDS");
+  __shared__ __align__(1024) char smem[L::LDS];
+
+  const int nvt = a.dv / BVS;
+  const int N = (a.T + C - 1) / C;
+  const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int hm = lb / nvt;
+  const int bh = (hm % a.B) * a.H + hm / a.B;
+  const int b = bh / a.H, h = bh % a.H;
+  const KeyHead kh = key_head(a.HK, a.H, h);
+  const Seq sq = seq_of(a.cu, b, a.T), sp = padded_rows(sq, b, a.T);
+  const int NLC = (sq.len + C - 1) / C;
+  const int l = lane_id(), g4 = l >> 4, c16 = l & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int v0 = (lb % nvt) * BVS;
+
+  if (w >= L::NC) {
+    // ---- loaders: wave 0 the keys, 1 and 2 half of the queries each, 3 X.  Rows
+    // past the end read the last row: P^T, Tm^T and the coefficients are zero there
+    // (those of dO are set to zero by the consumers).  A wave waits for all its loads.
+#define CCQ_LDS(src, dst) __builtin_amdgcn_global_load_lds((const void*)(src), (lds_void*)(dst), 16, 0, 0)
+    const int lw = w - L::NC;
+    constexpr int CPK = DK / 8, CPV = BVS / 8, R = 64 / CPK, NP = 16 / R, RV = 64 / CPV;
+    const size_t pitch = (size_t)kh.H * RB, vpitch = (size_t)a.H * a.dv * 2;
+    uint32_t lane[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      lane[p] = (l / CPK) * (uint32_t)pitch + 16 * ((l % CPK) ^ dswz<DK>(p * R + l / CPK));
+    // loads i0 .. i1 of the [C, DK] tile of chunk ci at base
+    auto rows = [&](const char* base, int ci, char* dst, int i0, auto n) {
+      const char* src = base + (size_t)ci * C * pitch;
+      const int nrow = sq.len - ci * C;
+      if (nrow >= C) {
+#pragma unroll
+        for (int i = 0; i < decltype(n)::value; ++i)
+          CCQ_LDS(src + (size_t)(i0 + i) * R * pitch + lane[i % NP], dst + (i0 + i) * 1024);
+      } else {
+#pragma unroll 1
+        for (int i = i0; i < i0 + decltype(n)::value; ++i) {
+          const int row = i * R + l / CPK;
+          CCQ_LDS(src + min(row, nrow - 1) * pitch + 16 * ((l % CPK) ^ dswz<DK>(row)), dst + i * 1024);
+        }
+      }
+    };
+    const size_t head = 2 * seq_off(sq, 0, kh.h, kh.H, DK);
+    if (lw == 0) {
+      const char* const kg = static_cast<const char*>(a.k) + head;
+      auto issue = [&](int ci) { rows(kg, ci, smem + (ci & 1) * L::KB, 0, std::integral_constant<int, L::NK>()); };
+      if (NLC > 0) issue(NLC - 1);
+#pragma unroll 1
+      for (int ci = NLC - 1; ci >= 0; --ci) {
+        wait_vm_all();
+        __builtin_amdgcn_s_barrier();
+        if (ci > 0) issue(ci - 1);
+        if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_s_barrier();
+      }
+    } else if (lw < 3) {
+      static_assert(L::NK / 2 % NP == 0, "half a tile begins a period of the permutation");
+      const char* const qg = static_cast<const char*>(a.qc) + head;
+#pragma unroll 1
+      for (int ci = NLC - 1; ci >= 0; --ci) {
+        __builtin_amdgcn_s_barrier();
+        rows(qg, ci, smem + L::QO, (lw - 1) * (L::NK / 2), std::integral_constant<int, L::NK / 2>());
+        if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
+        wait_vm_all();
+        __builtin_amdgcn_s_barrier();
+      }
+    } else {
+      const char* const og = static_cast<const char*>(a.dO) + 2 * (seq_off(sq, 0, h, a.H, a.dv) + v0);
+      const char* const pg = static_cast<const char*>(a.PT) + (size_t)bh * N * L::TB;
+      const char* const tg = static_cast<const char*>(a.TmT) + (size_t)bh * N * L::TB;
+      const float* const fg = a.gam + (size_t)bh * N * 5 * C;
+      const uint32_t vlane = (l / CPV) * (uint32_t)vpitch + 16 * (l % CPV);
+      const uint32_t tlane[2] = {(uint32_t)(16 * (l & ~7) + 16 * ((l % 8) ^ tswz(l / 8))),
+                                 (uint32_t)(16 * (l & ~7) + 16 * ((l % 8) ^ tswz(8 + l / 8)))};
+      auto issue = [&](int ci) {
+        char* sb = smem + L::XO + (ci & 1) * L::XB;
+        const char* oc = og + (size_t)ci * C * vpitch;
+        const int nrow = sq.len - ci * C;
+        CCQ_LDS(fg + (size_t)ci * 5 * C + 4 * l, sb + 2 * L::TB + L::VB);
+        if (l < 16) CCQ_LDS(fg + ((size_t)ci * 5 + 4) * C + 4 * l, sb + 2 * L::TB + L::VB + 1024);
+        if (nrow >= C) {
+#pragma unroll
+          for (int i = 0; i < L::NV; ++i) CCQ_LDS(oc + i * RV * vpitch + vlane, sb + 2 * L::TB + i * 1024);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < L::NV; ++i)
+            CCQ_LDS(oc + min(i * RV + l / CPV, nrow - 1) * vpitch + 16 * (l % CPV), sb + 2 * L::TB + i * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < L::NT; ++i) {
+          CCQ_LDS(pg + (size_t)ci * L::TB + i * 1024 + tlane[i % 2], sb + i * 1024);
+          CCQ_LDS(tg + (size_t)ci * L::TB + i * 1024 + tlane[i % 2], sb + L::TB + i * 1024);
+        }
+      };
+      if (NLC > 0) issue(NLC - 1);
+#pragma unroll 1
+      for (int ci = NLC - 1; ci >= 0; --ci) {
+        wait_vm_all();
+        __builtin_amdgcn_s_barrier();
+        if (ci > 0) issue(ci - 1);
+        if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_s_barrier();
+      }
+    }
+    return;
+#undef CCQ_LDS
+  }
+
+  // ---- consumer wave: features c0 .. of value tile pr of the workgroup's slice ----
+  const int pr = w / NH, hq = w % NH, c0 = hq * DKH;
+  const int v = v0 + 16 * pr + c16;
+  f32x4 D[NCT];  // D^T[c][v] in pair order: c = c0 + pair_feat(tc, g4) + r
+#pragma unroll
+  for (int tc = 0; tc < NCT; ++tc) D[tc] = zero4();
+  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+  auto ldf = [](const char* p) {
+    Frag<T> f;
+    f.v = *reinterpret_cast<const bf16x8*>(p);
+    return f;
+  };
+  auto tr = [](const char* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p); };
+  auto pair = [](bf16x4 lo, bf16x4 hi) {
+    Frag<T> f;
+    f.v = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return f;
+  };
+  // offsets into the K and Q tiles, as in the state pass
+  constexpr int NQ = NKH < 4 ? NKH : 4;
+  int krow[NQ], kcol[NQ];
+  {
+    const int rr = 4 * g4 + (c16 >> 2);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int M = c0 / 32 + q;
+      krow[q] = c16 * RB + (M >> 2) * 256 + 16 * ((4 * (M & 3) + g4) ^ dswz<DK>(c16));
+      kcol[q] = rr * RB + (M >> 2) * 256 + 16 * ((4 * (M & 3) + (c16 & 3)) ^ dswz<DK>(rr));
+    }
+  }
+  const int trow = c16 * (C * 2) + 16 * (g4 ^ tswz(c16));  // Tm^T row c16, slots 8 g4 ..; 32 on: ^ 64
+  // P^T row c16 in accumulator order: columns 4 g4 .. and 16 + 4 g4 .. (32 on: ^ 64)
+  const int prow = c16 * (C * 2) + 8 * (g4 & 1) + 16 * ((g4 >> 1) ^ tswz(c16)), prow2 = prow ^ 32;
+  const int vrow = (4 * g4 + (c16 >> 2)) * (2 * BVS) + 32 * pr + 8 * (c16 & 3);
+  f32x4* const sX = reinterpret_cast<f32x4*>(smem + L::SO);
+  T* const dst = static_cast<T*>(a.dstates) + ((size_t)bh * N * a.dv + v) * DK + c0 + 8 * g4;
+  T* const dRg = static_cast<T*>(a.dR) + v;
+  const int dpitch = a.H * a.dv;
+
+#pragma unroll 1
+  for (int ci = NLC - 1; ci >= 0; --ci) {
+    const char* kb = smem + (ci & 1) * L::KB;
+    const char* qb = smem + L::QO;
+    const char* pb = smem + L::XO + (ci & 1) * L::XB;
+    const char* tb = pb + L::TB;
+    const char* ob = tb + L::TB;
+    const float* Fb = reinterpret_cast<const float*>(ob + L::VB);
+    const int nrow = min(C, sq.len - ci * C);
+    Frag<T> df[NKH];
+#pragma unroll
+    for (int m = 0; m < NKH; ++m) df[m] = acc_pair_frag<T>(D[2 * m], D[2 * m + 1]);
+    lds_barrier();  // K and X have landed; Q's slot and the others' second ones are free
+    // partial dU: K D^T over the wave's features, and P^T dO for its share of the
+    // token tiles; LDS reads run a group ahead of their products
+    constexpr int GB = NKH < 4 ? NKH : 4, NGB = NKH / GB;
+    Frag<T> kf[2][GB];
+    auto read_k = [&](int step) {
+      const int J = step / NGB, m0 = (step % NGB) * GB;
+#pragma unroll
+      for (int m = 0; m < GB; ++m)
+        kf[step & 1][m] = ldf(kb + krow[(m0 + m) & 3] + ((m0 + m) >> 2) * 256 + 16 * J * RB);
+    };
+    read_k(0);
+    Frag<T> of[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) of[q] = pair(tr(ob + vrow + 32 * q * 2 * BVS), tr(ob + vrow + (32 * q + 16) * 2 * BVS));
+    {  // D, as it enters the chunk
+      T* out = dst + (size_t)ci * a.dv * DK;
+#pragma unroll
+      for (int m = 0; m < NKH; ++m) store_frag(out + 32 * m, df[m]);
+    }
+    const float eC = Fb[4 * C];
+    f32x4 dU[4];
+    Frag<T> tt[4][2];
+#pragma unroll
+    for (int J = 0; J < 4; ++J) {
+      f32x4 x[2] = {zero4(), zero4()};
+      Frag<T> pf[2];
+      const bool mine = J % NH == hq;
+#pragma unroll
+      for (int gb = 0; gb < NGB; ++gb) {
+        const int step = J * NGB + gb;
+        if (step + 1 < 4 * NGB) read_k(step + 1);
+        if (gb == NGB - 1) {
+          if (mine) {  // (P^T is zero left of the diagonal tiles)
+            auto half = [&](int q) {
+              return pair(*reinterpret_cast<const bf16x4*>(pb + (prow ^ (64 * q)) + 16 * J * (C * 2)),
+                          *reinterpret_cast<const bf16x4*>(pb + (prow2 ^ (64 * q)) + 16 * J * (C * 2)));
+            };
+            if (J < 2) pf[0] = half(0);
+            pf[1] = half(1);
+          }
+          if (J < 2) tt[J][0] = ldf(tb + trow + 16 * J * (C * 2));
+          tt[J][1] = ldf(tb + (trow ^ 64) + 16 * J * (C * 2));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < GB; ++m) mma(x[m & 1], kf[step & 1][m], df[gb * GB + m]);
+      }
+      const f32x4 cf = *reinterpret_cast<const f32x4*>(Fb + 3 * C + 16 * J + 4 * g4);
+      dU[J] = cf * (x[0] + x[1]);
+      if (mine) {
+        f32x4 y = zero4();
+        if (J < 2) mma(y, pf[0], of[0]);
+        mma(y, pf[1], of[1]);
+        dU[J] += a.scale * y;
+      }
+      if constexpr (NH > 1) sX[(w * 4 + J) * 64 + l] = dU[J];
+    }
+    // s e^gamma dO (zero past the end), and the first K^T tiles of the update
+    Frag<T> og[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      f32x4 lo = *reinterpret_cast<const f32x4*>(Fb + 32 * q + 4 * g4);
+      f32x4 hi = *reinterpret_cast<const f32x4*>(Fb + 32 * q + 16 + 4 * g4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        lo[r] = 32 * q + 4 * g4 + r < nrow ? a.scale * __expf(lo[r]) * frag_elem(of[q], r) : 0.f;
+        hi[r] = 32 * q + 16 + 4 * g4 + r < nrow ? a.scale * __expf(hi[r]) * frag_elem(of[q], 4 + r) : 0.f;
+      }
+      og[q] = acc_pair_frag<T>(lo, hi);
+    }
+    constexpr int TB = NCT < 4 ? NCT : 4;
+    Frag<T> tf[2][TB][2];
+    auto read_t = [&](const char* base, int tc0, Frag<T>(&f)[TB][2]) {
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        const int tc = tc0 + t, m = tc >> 1;
+        const char* p = base + kcol[m & 3] + (m >> 2) * 256 + 8 * (tc & 1);
+#pragma unroll
+        for (int kq = 0; kq < 2; ++kq) f[t][kq] = pair(tr(p + 32 * kq * RB), tr(p + (32 * kq + 16) * RB));
+      }
+    };
+    read_t(kb, 0, tf[0]);
+    if constexpr (NH > 1) {
+      lds_barrier();
+      // the tile's partial sums in a fixed order: its waves hold the same bits
+#pragma unroll
+      for (int J = 0; J < 4; ++J) {
+        f32x4 sum = sX[(pr * NH * 4 + J) * 64 + l];
+#pragma unroll
+        for (int hh = 1; hh < NH; ++hh) sum += sX[((pr * NH + hh) * 4 + J) * 64 + l];
+        dU[J] = sum;
+      }
+    }
+    f32x4 bg[4];
+#pragma unroll
+    for (int I = 0; I < 4; ++I) bg[I] = *reinterpret_cast<const f32x4*>(Fb + C + 16 * I + 4 * g4);
+    const Frag<T> uf0 = acc_pair_frag<T>(dU[0], dU[1]), uf1 = acc_pair_frag<T>(dU[2], dU[3]);
+    f32x4 dR[4];
+#pragma unroll
+    for (int I = 0; I < 4; ++I) {
+      dR[I] = zero4();
+      mma(dR[I], tt[I][1], uf1);
+    }
+#pragma unroll
+    for (int I = 0; I < 2; ++I) mma(dR[I], tt[I][0], uf0);
+#pragma unroll
+    for (int t = 0; t < NCT; ++t) D[t] *= eC;
+    T* const dRrow = dRg + seq_off(sp, ci * C, h, a.H, a.dv);
+#pragma unroll
+    for (int I = 0; I < 4; ++I) {
+      if (I % NH == hq)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * I + 4 * g4 + r;
+          if (i < nrow) dRrow[i * dpitch] = to<T>(dR[I][r]);
+        }
+      dR[I] *= -bg[I];
+    }
+    const Frag<T> rf[2] = {acc_pair_frag<T>(dR[0], dR[1]), acc_pair_frag<T>(dR[2], dR[3])};
+#pragma unroll
+    for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {
+      if (tb4 + 1 < NCT / TB) read_t(kb, TB * (tb4 + 1), tf[(tb4 + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) mma(D[TB * tb4 + t], tf[tb4 & 1][t][kq], rf[kq]);
+    }
+    lds_barrier();  // Q has landed
+    read_t(qb, 0, tf[0]);
+#pragma unroll
+    for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {
+      if (tb4 + 1 < NCT / TB) read_t(qb, TB * (tb4 + 1), tf[(tb4 + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) mma(D[TB * tb4 + t], tf[tb4 & 1][t][kq], og[kq]);
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------
 // Recurrent form on the fp32 state, in place, for one or a few tokens:
 //   u = beta (v - alpha S k),  o = scale (alpha S q + (k . q) u),  S <- alpha S + u k^T.
 // Every row of S goes through the tokens on its own, so a row is read once and
@@ -516,6 +853,27 @@ hipError_t run_delta_state_dk(const GdnArgs& a, hipStream_t st) {
     else return run_delta_state<DK, 2, 1>(a, st);
   }
 }
+template <int DK, int NPR, int NH>
+hipError_t run_delta_dstate(const GdnDstateArgs& a, hipStream_t st) {
+  typedef DeltaBackTile<DK, NPR, NH> L;
+  const int nblk = a.B * a.H * (a.dv / (16 * NPR));
+  if (nblk == 0) return hipSuccess;
+  hipLaunchKernelGGL((delta_dstate_kernel<DK, NPR, NH>), dim3(nblk), dim3(64 * (L::NC + L::NLW)), 0, st, a);
+  return hipGetLastError();
+}
+template <int DK>
+hipError_t run_delta_dstate_dk(const GdnDstateArgs& a, hipStream_t st) {
+  const long long tiles = (long long)a.B * a.H * (a.dv / 16);
+  if constexpr (DK == 64) {
+    if (tiles > 512) return run_delta_dstate<DK, 4, 1>(a, st);
+    return run_delta_dstate<DK, 2, 1>(a, st);
+  } else {
+    if (tiles <= 256) return run_delta_dstate<DK, 1, 4>(a, st);
+    if (DK == 256 || tiles <= 512) return run_delta_dstate<DK, 2, 2>(a, st);
+    if constexpr (DK == 128) return run_delta_dstate<DK, 4, 1>(a, st);
+    return hipErrorInvalidValue;
+  }
+}
 template <typename T>
 hipError_t step_dispatch(const DeltaStepArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.HV * (a.dv / kStepRows))), block(kStepThreads);
@@ -534,6 +892,15 @@ hipError_t launch_delta_state(const GdnArgs& a, hipStream_t st) {
     case 64: return run_delta_state_dk<64>(a, st);
     case 128: return run_delta_state_dk<128>(a, st);
     case 256: return run_delta_state_dk<256>(a, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_delta_dstate(const GdnDstateArgs& a, hipStream_t st) {
+  switch (a.dk) {
+    case 64: return run_delta_dstate_dk<64>(a, st);
+    case 128: return run_delta_dstate_dk<128>(a, st);
+    case 256: return run_delta_dstate_dk<256>(a, st);
   }
   return hipErrorInvalidValue;
 }

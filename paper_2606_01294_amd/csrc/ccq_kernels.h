@@ -452,7 +452,8 @@ hipError_t launch_gdn_tri(const TriArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_gdn_state(const GdnArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_gdn_state_roles(const GdnArgs& a, hipStream_t st);  // bf16, dk = 128 or 256
 hipError_t launch_gdn_out(const GdnOutArgs& a, bool is_bf16, hipStream_t st);
-hipError_t launch_delta_state(const GdnArgs& a, hipStream_t st);  // bf16
+hipError_t launch_delta_state(const GdnArgs& a, hipStream_t st);         // bf16
+hipError_t launch_delta_dstate(const GdnDstateArgs& a, hipStream_t st);  // bf16
 hipError_t launch_delta_step(const DeltaStepArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_head_sum(const HeadSumArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_copy_or_zero(float* dst, const float* src, size_t n, hipStream_t st);

@@ -134,7 +134,9 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
                         s->scale};
   da.cu = cu;
   da.HK = s->HK;
-  if (traced(st, [&] { return ccq::launch_gdn_dstate(da, bf, st); }) != hipSuccess) return CCQ_ERR_HIP;
+  if (traced(st, [&] { return bf ? ccq::launch_delta_dstate(da, st) : ccq::launch_gdn_dstate(da, false, st); }) !=
+      hipSuccess)
+    return CCQ_ERR_HIP;
   ccq::GdnBwdArgs ba{};
   ba.qc = q;
   ba.k = k;
