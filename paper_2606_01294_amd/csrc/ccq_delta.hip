@@ -416,15 +416,21 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 // consumer waves a value tile of 16 columns of D^T, the features of a tile split
 // over them (one exchange of the partial dU), four waves that only stream.  K and
 // X (P^T, Tm^T, dO, coefficients) come one chunk ahead into two slots each; Q, which
-// only the end of a chunk reads, into one: its loads go out when the chunk begins
-// and a barrier of its own stands before its products.  Operands are bf16, D and
-// every sum fp32 (D and dR are rounded as operands and on store).
+// only the end of a chunk reads, into one: its loads go out when the chunk begins, as
+// those of X, those of K behind the exchange (a wave with that many loads to issue
+// would hold the barrier there: 127 against 105 us at 512 tiles of dk = 128 with all
+// three behind it, 109 with all before), and a barrier stands before Q's products.
+// dR leaves through LDS and a loader: stored by the consumers themselves, two bytes a
+// lane and row, it held them up.  Operands are bf16, D and every sum fp32 (D and dR
+// are rounded as operands and on store).
+// 1.3B training step (B = 4, T = 4096, H = 8, dk = dv = 256): 335 us in the form of
+// gdn_dstate_kernel, which stages through registers, 225 in this one.
 template <int DK, int NPR, int NH>
 struct DeltaBackTile {
   static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NC = NPR * NH;
   static constexpr int KB = C * DK * 2, TB = C * C * 2, VB = C * BVS * 2, FB = 5 * C * 4;
   static constexpr int XB = 2 * TB + VB + FB, SB = NH > 1 ? NC * 4 * 64 * 16 : 0;
-  static constexpr int QO = 2 * KB, XO = QO + KB, SO = XO + 2 * XB, LDS = SO + SB;
+  static constexpr int QO = 2 * KB, XO = QO + KB, SO = XO + 2 * XB, RO = SO + SB, LDS = RO + VB;
   static constexpr int NK = KB / 1024, NT = TB / 1024, NV = VB / 1024;  // 1 KB loads
 };
 
@@ -453,8 +459,7 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 
   if (w >= L::NC) {
     // ---- loaders: wave 0 the keys, 1 and 2 half of the queries each, 3 X.  Rows
-    // past the end read the last row: P^T, Tm^T and the coefficients are zero there
-    // (those of dO are set to zero by the consumers).  A wave waits for all its loads.
+    // past the end read the last row: P^T, Tm^T and the coefficients are zero there.  A wave waits for all its loads.
 #define CCQ_LDS(src, dst) __builtin_amdgcn_global_load_lds((const void*)(src), (lds_void*)(dst), 16, 0, 0)
     const int lw = w - L::NC;
     constexpr int CPK = DK / 8, CPV = BVS / 8, R = 64 / CPK, NP = 16 / R, RV = 64 / CPV;
@@ -488,8 +493,8 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
       for (int ci = NLC - 1; ci >= 0; --ci) {
         wait_vm_all();
         __builtin_amdgcn_s_barrier();
-        if (ci > 0) issue(ci - 1);
         if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
+        if (ci > 0) issue(ci - 1);
         __builtin_amdgcn_s_barrier();
       }
     } else if (lw < 3) {
@@ -502,6 +507,16 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
         if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
         wait_vm_all();
         __builtin_amdgcn_s_barrier();
+        if (lw == 1) {  // the chunk's dR (whole rows of the slice), out of the consumers' way
+          const int nrow = sq.len - ci * C;
+          char* const out = static_cast<char*>(a.dR) + 2 * (seq_off(sp, ci * C, h, a.H, a.dv) + v0);
+#pragma unroll
+          for (int i = 0; i < L::NV; ++i) {
+            const int row = i * RV + l / CPV;
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(smem + L::RO + i * 1024 + 16 * l);
+            if (row < nrow) *reinterpret_cast<bf16x8*>(out + row * vpitch + 16 * (l % CPV)) = x;
+          }
+        }
       }
     } else {
       const char* const og = static_cast<const char*>(a.dO) + 2 * (seq_off(sq, 0, h, a.H, a.dv) + v0);
@@ -535,7 +550,10 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 #pragma unroll 1
       for (int ci = NLC - 1; ci >= 0; --ci) {
         wait_vm_all();
-        __builtin_amdgcn_s_barrier();
+        // s e^gamma, zero past the end, over gamma
+        float* const F = reinterpret_cast<float*>(smem + L::XO + (ci & 1) * L::XB + 2 * L::TB + L::VB);
+        F[l] = l < sq.len - ci * C ? a.scale * __expf(F[l]) : 0.f;
+        lds_barrier();
         if (ci > 0) issue(ci - 1);
         if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_s_barrier();
@@ -547,7 +565,6 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 
   // ---- consumer wave: features c0 .. of value tile pr of the workgroup's slice ----
   const int pr = w / NH, hq = w % NH, c0 = hq * DKH;
-  const int v = v0 + 16 * pr + c16;
   f32x4 D[NCT];  // D^T[c][v] in pair order: c = c0 + pair_feat(tc, g4) + r
 #pragma unroll
   for (int tc = 0; tc < NCT; ++tc) D[tc] = zero4();
@@ -580,9 +597,8 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
   const int prow = c16 * (C * 2) + 8 * (g4 & 1) + 16 * ((g4 >> 1) ^ tswz(c16)), prow2 = prow ^ 32;
   const int vrow = (4 * g4 + (c16 >> 2)) * (2 * BVS) + 32 * pr + 8 * (c16 & 3);
   f32x4* const sX = reinterpret_cast<f32x4*>(smem + L::SO);
-  T* const dst = static_cast<T*>(a.dstates) + ((size_t)bh * N * a.dv + v) * DK + c0 + 8 * g4;
-  T* const dRg = static_cast<T*>(a.dR) + v;
-  const int dpitch = a.H * a.dv;
+  T* const dst = static_cast<T*>(a.dstates) + ((((size_t)bh * N * (a.dv / 16) + (v0 >> 4) + pr) * (DK / 32) + hq * NKH) * 16 + c16) * 32 + 8 * g4;
+  char* const rrow = smem + L::RO + (4 * g4 + 2 * (c16 & 1)) * 2 * BVS + 32 * pr + 2 * (c16 & ~1);
 
 #pragma unroll 1
   for (int ci = NLC - 1; ci >= 0; --ci) {
@@ -592,7 +608,6 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
     const char* tb = pb + L::TB;
     const char* ob = tb + L::TB;
     const float* Fb = reinterpret_cast<const float*>(ob + L::VB);
-    const int nrow = min(C, sq.len - ci * C);
     Frag<T> df[NKH];
 #pragma unroll
     for (int m = 0; m < NKH; ++m) df[m] = acc_pair_frag<T>(D[2 * m], D[2 * m + 1]);
@@ -611,10 +626,10 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
     Frag<T> of[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) of[q] = pair(tr(ob + vrow + 32 * q * 2 * BVS), tr(ob + vrow + (32 * q + 16) * 2 * BVS));
-    {  // D, as it enters the chunk
+    {  // D, as it enters the chunk, fragment-native
       T* out = dst + (size_t)ci * a.dv * DK;
 #pragma unroll
-      for (int m = 0; m < NKH; ++m) store_frag(out + 32 * m, df[m]);
+      for (int m = 0; m < NKH; ++m) store_frag(out + 16 * 32 * m, df[m]);
     }
     const float eC = Fb[4 * C];
     f32x4 dU[4];
@@ -654,7 +669,7 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
       }
       if constexpr (NH > 1) sX[(w * 4 + J) * 64 + l] = dU[J];
     }
-    // s e^gamma dO (zero past the end), and the first K^T tiles of the update
+    // s e^gamma dO, and the first K^T tiles of the update
     Frag<T> og[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -662,8 +677,8 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
       f32x4 hi = *reinterpret_cast<const f32x4*>(Fb + 32 * q + 16 + 4 * g4);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        lo[r] = 32 * q + 4 * g4 + r < nrow ? a.scale * __expf(lo[r]) * frag_elem(of[q], r) : 0.f;
-        hi[r] = 32 * q + 16 + 4 * g4 + r < nrow ? a.scale * __expf(hi[r]) * frag_elem(of[q], 4 + r) : 0.f;
+        lo[r] *= frag_elem(of[q], r);
+        hi[r] *= frag_elem(of[q], 4 + r);
       }
       og[q] = acc_pair_frag<T>(lo, hi);
     }
@@ -704,18 +719,10 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
     for (int I = 0; I < 2; ++I) mma(dR[I], tt[I][0], uf0);
 #pragma unroll
     for (int t = 0; t < NCT; ++t) D[t] *= eC;
-    T* const dRrow = dRg + seq_off(sp, ci * C, h, a.H, a.dv);
+    f32x4 dRb[4];
 #pragma unroll
-    for (int I = 0; I < 4; ++I) {
-      if (I % NH == hq)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = 16 * I + 4 * g4 + r;
-          if (i < nrow) dRrow[i * dpitch] = to<T>(dR[I][r]);
-        }
-      dR[I] *= -bg[I];
-    }
-    const Frag<T> rf[2] = {acc_pair_frag<T>(dR[0], dR[1]), acc_pair_frag<T>(dR[2], dR[3])};
+    for (int I = 0; I < 4; ++I) dRb[I] = dR[I] * -bg[I];
+    const Frag<T> rf[2] = {acc_pair_frag<T>(dRb[0], dRb[1]), acc_pair_frag<T>(dRb[2], dRb[3])};
 #pragma unroll
     for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {
       if (tb4 + 1 < NCT / TB) read_t(kb, TB * (tb4 + 1), tf[(tb4 + 1) & 1]);
@@ -725,7 +732,21 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 #pragma unroll
         for (int t = 0; t < TB; ++t) mma(D[TB * tb4 + t], tf[tb4 & 1][t][kq], rf[kq]);
     }
-    lds_barrier();  // Q has landed
+    // dR to LDS, token-major: a lane holds four tokens of one column; neighbours
+    // swap two of them, so that each writes two tokens of two columns
+#pragma unroll
+    for (int I = 0; I < 4; ++I)
+      if (I % NH == hq) {
+        typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+        const bool odd = c16 & 1;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float keep = odd ? dR[I][2 + r] : dR[I][r], give = odd ? dR[I][r] : dR[I][2 + r];
+          const float got = __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, give), 0xB1, 0xf, 0xf, true));
+          *reinterpret_cast<bf16x2*>(rrow + (16 * I + r) * 2 * BVS) = bf16x2{to<T>(odd ? got : keep), to<T>(odd ? keep : got)};
+        }
+      }
+    lds_barrier();  // Q has landed, dR is in LDS
     read_t(qb, 0, tf[0]);
 #pragma unroll
     for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {

@@ -361,6 +361,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   constexpr int LDQ = DK + P, LDT = C + P, LDV = BV + P;
   constexpr int NTC = DK / 16, NTW = NTC / HW;  // key-channel tiles, per wave
   constexpr int ES = (int)sizeof(T);
+  constexpr bool kFragD = PLAIN && sizeof(T) == 2;  // the plain rule's bf16 scan stores D as S_r is stored
   static_assert(BV % 32 == 0 && DK % 32 == 0, "tiles");
   static_assert((NW == 4 || NW == 8) && NTW * HW == NTC, "wave split");
 
@@ -460,7 +461,8 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         const int m = rem / 64, vr = (rem % 64) / 4, pp = rem % 4;
         sl.s[p] = *reinterpret_cast<const v8*>(Sg + (size_t)(vv0 / 16 + vt) * 16 * DK + (size_t)(m * 16 + vr) * 32 + 8 * pp);
         const int vd = q / (DK / 8), cd = (q % (DK / 8)) * 8;
-        sl.d[p] = *reinterpret_cast<const v8*>(Dg + (size_t)(vv0 + vd) * DK + cd);
+        sl.d[p] = kFragD ? *reinterpret_cast<const v8*>(Dg + (size_t)(vv0 / 16 + vt) * 16 * DK + (size_t)(m * 16 + vr) * 32 + 8 * pp)
+                         : *reinterpret_cast<const v8*>(Dg + (size_t)(vv0 + vd) * DK + cd);
       }
 #pragma unroll
       for (int p = 0; p < NPU; ++p) {
@@ -503,7 +505,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         const int m = rem / 64, vr = (rem % 64) / 4, pp = rem % 4;
         const int vl = 16 * vt + vr;
         *reinterpret_cast<v8*>(sS + vl * LDQ + 32 * m + 8 * pp) = cur.s[p];
-        const int vd = q / (DK / 8), cd = (q % (DK / 8)) * 8;
+        const int vd = kFragD ? vl : q / (DK / 8), cd = kFragD ? 32 * m + 8 * pp : (q % (DK / 8)) * 8;
         *reinterpret_cast<v8*>(sD + vd * LDQ + cd) = cur.d[p];
       }
 #pragma unroll

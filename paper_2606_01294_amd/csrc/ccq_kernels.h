@@ -253,7 +253,7 @@ struct GdnDstateArgs {
   const float* gam;      // forward workspace, as TriArgs
   const void* PT;        // as GdnPrepArgs
   const void* TmT;       // as GdnPrepArgs
-  void* dstates;         // [B*H, N, dv, dk] io, plain row-major
+  void* dstates;         // [B*H, N, dv, dk] io, plain row-major (the plain rule, bf16: fragment-native, as GdnArgs)
   void* dR;              // [B,T,H,dv] io
   int B, T, H, dk, dv;
   float scale;
