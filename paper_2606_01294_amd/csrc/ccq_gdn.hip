@@ -449,7 +449,11 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
 // the lane's entries of two pair-ordered accumulator tiles (tiles 2m, 2m + 1
 // of ld_frag_tr_acc_pair), so the update unpacks, accumulates and repacks in
 // place.
-template <typename T, int DK, int VPW, int IPW, bool CARRY>
+//
+// PAIR (the plain rule, bf16): the scores enter the product with U as a bf16 head
+// and tail, one rounding fewer in o (2.5e-3 instead of 3.0e-3 from the exact result
+// at the 1.3B shape, a stored bf16 value's own rounding being 1.7e-3).
+template <typename T, int DK, int VPW, int IPW, bool CARRY, bool PAIR>
 __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArgs a) {
   constexpr int C = kChunk;
   constexpr int P = Pad<T>::value;
@@ -462,6 +466,7 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
   __shared__ __align__(16) T sQ[C * LDQ];
   __shared__ __align__(16) T sK[C * LDQ];
   __shared__ __align__(16) T sP[C * LDP];  // P[i][acc_pos(j)]
+  __shared__ __align__(16) T sPl[PAIR ? C * LDP : 1];  // what its rounding left
   __shared__ __align__(16) float sGam[C];
   __shared__ __align__(16) float sDd[C + 4];  // e^{gamma_C - gamma_j}; e^{gamma_C} at C
   __shared__ float sRk[C];                    // raw keys: row scales of the scores
@@ -540,6 +545,11 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
         }
       }
       store4(sP + i * LDP + acc_pos(16 * J + 4 * g4), x[0], x[1], x[2], x[3]);
+      if constexpr (PAIR) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] -= f32(to<T>(x[r]));
+        store4(sPl + i * LDP + acc_pos(16 * J + 4 * g4), x[0], x[1], x[2], x[3]);
+      }
     }
     lds_barrier();
 
@@ -559,10 +569,19 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
       }
       const Frag<T> pf0 = ld_frag(sP + 16 * I * LDP, LDP);
       const Frag<T> pf1 = ld_frag(sP + 16 * I * LDP + 32, LDP);
+      Frag<T> pl0, pl1;
+      if constexpr (PAIR) {
+        pl0 = ld_frag(sPl + 16 * I * LDP, LDP);
+        pl1 = ld_frag(sPl + 16 * I * LDP + 32, LDP);
+      }
       const float ei = __expf(sGam[i]);
 #pragma unroll
       for (int vt = 0; vt < VPW; ++vt) {
         acc[vt] *= ei;
+        if constexpr (PAIR) {
+          mma(acc[vt], ufr[vt][0], pl0);
+          if (I >= 2) mma(acc[vt], ufr[vt][1], pl1);
+        }
         mma(acc[vt], ufr[vt][0], pf0);
         if (I >= 2) mma(acc[vt], ufr[vt][1], pf1);  // keys 32..63 precede row i only for I >= 2
         if (i < nrow) {
@@ -665,7 +684,10 @@ hipError_t run_gdn_out_v(const GdnOutArgs& a, hipStream_t st) {
   const int N = (a.T + kChunk - 1) / kChunk;
   const int nblk = a.B * a.H * ((N + a.group - 1) / a.group);
   if (nblk == 0) return hipSuccess;
-  hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry>), dim3(nblk), dim3(kOutThreads), 0, st, a);
+  if (a.HK && sizeof(T) == 2)
+    hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry, sizeof(T) == 2>), dim3(nblk), dim3(kOutThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry, false>), dim3(nblk), dim3(kOutThreads), 0, st, a);
   return hipGetLastError();
 }
 template <typename T, int DK>
