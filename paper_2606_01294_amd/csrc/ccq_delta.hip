@@ -742,7 +742,7 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float keep = odd ? dR[I][2 + r] : dR[I][r], give = odd ? dR[I][r] : dR[I][2 + r];
-          const float got = __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, give), 0xB1, 0xf, 0xf, true));
+          const float got = lane_swap(give);
           *reinterpret_cast<bf16x2*>(rrow + (16 * I + r) * 2 * BVS) = bf16x2{to<T>(odd ? got : keep), to<T>(odd ? keep : got)};
         }
       }

@@ -732,6 +732,11 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
+// The value of the neighbouring lane (lane ^ 1).
+__device__ __forceinline__ float lane_swap(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));
+}
+
 // Scalar per-token value prefetched by lane `row` (clamped address, zeroed at use).
 struct RowScalar {
   float x;
