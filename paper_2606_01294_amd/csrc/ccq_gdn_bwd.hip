@@ -373,7 +373,11 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   __shared__ float sRed[2][NW];
   __shared__ float sHalf[HW > 1 ? 6 : 1][C];  // the second half's per-row sums
   constexpr int kR2 = 4 * C * LDV * ES + 2 * BV * LDQ * ES;
-  constexpr int kR3 = 2 * C * LDT * ES;
+  // the plain rule, bf16: the C x C weights of dQ and dK as a head and a tail.  A
+  // rounded weight is off by the same factor for a whole row (for one token: for the
+  // whole of dk, up to 2^-8), where q and k themselves are exact
+  constexpr bool kPair = PLAIN && sizeof(T) == 2;
+  constexpr int kR3 = (kPair ? 4 : 2) * C * LDT * ES;
   constexpr int kR = kR2 > kR3 ? kR2 : kR3;
   __shared__ __align__(16) char sR[kR];
 
@@ -569,6 +573,8 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   // ---- phase 3: C x C weights
   T* sPm = reinterpret_cast<T*>(sR);  // rows i (the products over i read it transposed)
   T* sE = sPm + C * LDT;
+  T* sPl = sE + C * LDT;  // (kPair: the tails)
+  T* sEl = sPl + C * LDT;
   float rowF[4] = {0.f, 0.f, 0.f, 0.f}, rowA[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int jj = 0; jj < NJ; ++jj) {
@@ -590,6 +596,10 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       colA += sBeta[i] * fa;
       sPm[i * LDT + j] = to<T>(pm);
       sE[i * LDT + j] = to<T>(E);
+      if constexpr (kPair) {
+        sPl[i * LDT + j] = to<T>(pm - f32(to<T>(pm)));
+        sEl[i * LDT + j] = to<T>(E - f32(to<T>(E)));
+      }
     }
     colF += __shfl_xor(colF, 16);
     colF += __shfl_xor(colF, 32);
@@ -620,6 +630,12 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
     tile_mma_tr<T, C>(y, sPm + 16 * sw, LDT, sQ + cc, LDQ);
     tile_mma_bt<T, C>(y, sE + 16 * sw * LDT, LDT, sK + cc, LDQ);
     tile_mma_tr<T, C>(y, sE + 16 * sw, LDT, sK + cc, LDQ);
+    if constexpr (kPair) {
+      tile_mma_bt<T, C>(x, sPl + 16 * sw * LDT, LDT, sK + cc, LDQ);
+      tile_mma_tr<T, C>(y, sPl + 16 * sw, LDT, sQ + cc, LDQ);
+      tile_mma_bt<T, C>(y, sEl + 16 * sw * LDT, LDT, sK + cc, LDQ);
+      tile_mma_tr<T, C>(y, sEl + 16 * sw, LDT, sK + cc, LDQ);
+    }
     const int c = cc + c16;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
