@@ -408,10 +408,10 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 // Reverse scan of D = dL/dS_{r+1} (bf16 io), last chunk to first, with dO the
 // upstream gradient and s the read scale (see ccq_gdn_bwd.hip):
 //
-//   dU = diag(e^{gamma_C - gamma}) K D^T + s P^T dO,   dR = Tm^T dU   (stored),
+//   dU = diag(e^{gamma_C - gamma}) K D^T + s P^T dO,   dR = Tm^T dU,   dV = diag(beta) dR,
 //   D <- e^{gamma_C} D + Q^T (s diag(e^gamma) dO) - K^T diag(beta e^gamma) dR.
 //
-// D (as it enters the chunk) and dR are stored for the chunk-parallel gradients.
+// dV is stored, and D (as it enters the chunk) and dR for the chunk-parallel gradients.
 // Bound, as the state pass, by the chain of chunks and laid out like it: NH
 // consumer waves a value tile of 16 columns of D^T, the features of a tile split
 // over them (one exchange of the partial dU), four waves that only stream.  K and
@@ -420,8 +420,8 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 // those of X, those of K behind the exchange (a wave with that many loads to issue
 // would hold the barrier there: 127 against 105 us at 512 tiles of dk = 128 with all
 // three behind it, 109 with all before), and a barrier stands before Q's products.
-// dR leaves through LDS and a loader: stored by the consumers themselves, two bytes a
-// lane and row, it held them up.  Operands are bf16, D and every sum fp32 (D and dR
+// dR and dV leave through LDS and two loaders: stored by the consumers themselves,
+// two bytes a lane and row, dR held them up.  Operands are bf16, D and every sum fp32 (D and dR
 // are rounded as operands and on store).
 // 1.3B training step (B = 4, T = 4096, H = 8, dk = dv = 256): 335 us in the form of
 // gdn_dstate_kernel, which stages through registers, 225 in this one.
@@ -430,7 +430,10 @@ struct DeltaBackTile {
   static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NC = NPR * NH;
   static constexpr int KB = C * DK * 2, TB = C * C * 2, VB = C * BVS * 2, FB = 5 * C * 4;
   static constexpr int XB = 2 * TB + VB + FB, SB = NH > 1 ? NC * 4 * 64 * 16 : 0;
-  static constexpr int QO = 2 * KB, XO = QO + KB, SO = XO + 2 * XB, RO = SO + SB, LDS = RO + VB;
+  static constexpr int QO = 2 * KB, XO = QO + KB, SO = XO + 2 * XB, RO = SO + SB;
+  // dR and dV on their way out: over P^T, which the exchange releases, or apart
+  static constexpr int LDS = RO + (NH > 1 ? 0 : 2 * VB);
+  static_assert(2 * VB <= TB || NH == 1, "dR and dV over P^T");
   static constexpr int NK = KB / 1024, NT = TB / 1024, NV = VB / 1024;  // 1 KB loads
 };
 
@@ -507,15 +510,16 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
         if constexpr (NH > 1) __builtin_amdgcn_s_barrier();
         wait_vm_all();
         __builtin_amdgcn_s_barrier();
-        if (lw == 1) {  // the chunk's dR (whole rows of the slice), out of the consumers' way
-          const int nrow = sq.len - ci * C;
-          char* const out = static_cast<char*>(a.dR) + 2 * (seq_off(sp, ci * C, h, a.H, a.dv) + v0);
+        // the chunk's dR (to the workspace) and dV (to the caller), whole rows of the slice
+        const int nrow = sq.len - ci * C;
+        char* const out = lw == 1 ? static_cast<char*>(a.dR) + 2 * (seq_off(sp, ci * C, h, a.H, a.dv) + v0)
+                                  : static_cast<char*>(a.dv_out) + 2 * (seq_off(sq, ci * C, h, a.H, a.dv) + v0);
+        const char* const from = smem + (NH > 1 ? L::XO + (ci & 1) * L::XB : L::RO) + (lw - 1) * L::VB + 16 * l;
 #pragma unroll
-          for (int i = 0; i < L::NV; ++i) {
-            const int row = i * RV + l / CPV;
-            const bf16x8 x = *reinterpret_cast<const bf16x8*>(smem + L::RO + i * 1024 + 16 * l);
-            if (row < nrow) *reinterpret_cast<bf16x8*>(out + row * vpitch + 16 * (l % CPV)) = x;
-          }
+        for (int i = 0; i < L::NV; ++i) {
+          const int row = i * RV + l / CPV;
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(from + i * 1024);
+          if (row < nrow) *reinterpret_cast<bf16x8*>(out + row * vpitch + 16 * (l % CPV)) = x;
         }
       }
     } else {
@@ -598,7 +602,7 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
   const int vrow = (4 * g4 + (c16 >> 2)) * (2 * BVS) + 32 * pr + 8 * (c16 & 3);
   f32x4* const sX = reinterpret_cast<f32x4*>(smem + L::SO);
   T* const dst = static_cast<T*>(a.dstates) + ((((size_t)bh * N * (a.dv / 16) + (v0 >> 4) + pr) * (DK / 32) + hq * NKH) * 16 + c16) * 32 + 8 * g4;
-  char* const rrow = smem + L::RO + (4 * g4 + 2 * (c16 & 1)) * 2 * BVS + 32 * pr + 2 * (c16 & ~1);
+  const int rrow = (4 * g4 + 2 * (c16 & 1)) * 2 * BVS + 32 * pr + 2 * (c16 & ~1);
 
 #pragma unroll 1
   for (int ci = NLC - 1; ci >= 0; --ci) {
@@ -732,21 +736,25 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 #pragma unroll
         for (int t = 0; t < TB; ++t) mma(D[TB * tb4 + t], tf[tb4 & 1][t][kq], rf[kq]);
     }
-    // dR to LDS, token-major: a lane holds four tokens of one column; neighbours
-    // swap two of them, so that each writes two tokens of two columns
+    // dR and dV to LDS, token-major: a lane holds four tokens of one column;
+    // neighbours swap two of them, so that each writes two tokens of two columns
+    char* const ro = smem + (NH > 1 ? L::XO + (ci & 1) * L::XB : L::RO) + rrow;
+    auto out = [&](const f32x4& x, char* to_) {
+      typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+      const bool odd = c16 & 1;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float keep = odd ? x[2 + r] : x[r], got = lane_swap(odd ? x[r] : x[2 + r]);
+        *reinterpret_cast<bf16x2*>(to_ + r * 2 * BVS) = bf16x2{to<T>(odd ? got : keep), to<T>(odd ? keep : got)};
+      }
+    };
 #pragma unroll
     for (int I = 0; I < 4; ++I)
       if (I % NH == hq) {
-        typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
-        const bool odd = c16 & 1;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float keep = odd ? dR[I][2 + r] : dR[I][r], give = odd ? dR[I][r] : dR[I][2 + r];
-          const float got = lane_swap(give);
-          *reinterpret_cast<bf16x2*>(rrow + (16 * I + r) * 2 * BVS) = bf16x2{to<T>(odd ? got : keep), to<T>(odd ? keep : got)};
-        }
+        out(dR[I], ro + 16 * I * 2 * BVS);
+        out(dR[I] * *reinterpret_cast<const f32x4*>(Fb + 2 * C + 16 * I + 4 * g4), ro + L::VB + 16 * I * 2 * BVS);
       }
-    lds_barrier();  // Q has landed, dR is in LDS
+    lds_barrier();  // Q has landed, dR and dV are in LDS
     read_t(qb, 0, tf[0]);
 #pragma unroll
     for (int tb4 = 0; tb4 < NCT / TB; ++tb4) {

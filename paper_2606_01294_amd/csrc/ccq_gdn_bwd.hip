@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   constexpr int LDQ = DK + P, LDT = C + P, LDV = BV + P;
   constexpr int NTC = DK / 16, NTW = NTC / HW;  // key-channel tiles, per wave
   constexpr int ES = (int)sizeof(T);
-  constexpr bool kFragD = PLAIN && sizeof(T) == 2;  // the plain rule's bf16 scan stores D as S_r is stored
+  constexpr bool kFragD = PLAIN && sizeof(T) == 2;  // the plain rule's bf16 scan stores D as S_r is stored, and dV
   static_assert(BV % 32 == 0 && DK % 32 == 0, "tiles");
   static_assert((NW == 4 || NW == 8) && NTW * HW == NTC, "wave split");
 
@@ -497,7 +497,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         *reinterpret_cast<v8*>(sdO + vrow * LDV + vcol) = yo;
         *reinterpret_cast<v8*>(sdR + vrow * LDV + vcol) = xr;
         *reinterpret_cast<v8*>(sV + vrow * LDV + vcol) = xv;
-        if (vrow < nrow) *reinterpret_cast<v8*>(dvrow + vrow * (int)gsv + vv0 + vcol) = yd;
+        if (!kFragD && vrow < nrow) *reinterpret_cast<v8*>(dvrow + vrow * (int)gsv + vv0 + vcol) = yd;
       }
       // S_r and U^T slices (fragment-native: per value tile and 32-wide k
       // block, 16 rows of 32; S_r rows in natural order, U^T rows in acc_pos

@@ -259,6 +259,7 @@ struct GdnDstateArgs {
   float scale;
   const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
   int HK = 0;               // as GdnOutArgs
+  void* dv_out = nullptr;   // the plain rule, bf16: dL/dv, the caller's rows
 };
 
 // Chunk-parallel Gated DeltaNet gradients given S_r, U, dS_{r+1} and dR.

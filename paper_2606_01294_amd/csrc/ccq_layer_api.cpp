@@ -134,6 +134,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
                         s->scale};
   da.cu = cu;
   da.HK = s->HK;
+  da.dv_out = g->dv;
   if (traced(st, [&] { return bf ? ccq::launch_delta_dstate(da, st) : ccq::launch_gdn_dstate(da, false, st); }) !=
       hipSuccess)
     return CCQ_ERR_HIP;
