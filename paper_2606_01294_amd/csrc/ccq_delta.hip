@@ -890,17 +890,23 @@ hipError_t run_delta_dstate(const GdnDstateArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((delta_dstate_kernel<DK, NPR, NH>), dim3(nblk), dim3(64 * (L::NC + L::NLW)), 0, st, a);
   return hipGetLastError();
 }
+// Value tiles a workgroup and waves a tile, as for the state pass (the scan alone,
+// 32 chunks):
+//   dk = 256:  128 tiles  65 us at 1 x 4 waves, 86 at 2 x 2;  512: 103 at 2 x 2, 145 at 1 x 4
+//   dk = 128:  128        55 at 1 x 4, 60 at 2 x 1;   512: 76 at 2 x 2 and at 2 x 1, 91 at 4 x 1;
+//             1024       112 at 4 x 1, 154 at 2 x 2, 161 at 8 x 1
+//   dk = 64:    64        53 at 2 x 1, 52 at 1 x 2;   512: 72 at 2 x 1, 79 at 4 x 1
+// and, with 16 chunks, 2048 tiles: 96 at 8 x 1, 112 at 4 x 1 (dk = 128), 74 and 91 (dk = 64).
 template <int DK>
 hipError_t run_delta_dstate_dk(const GdnDstateArgs& a, hipStream_t st) {
   const long long tiles = (long long)a.B * a.H * (a.dv / 16);
-  if constexpr (DK == 64) {
-    if (tiles > 512) return run_delta_dstate<DK, 4, 1>(a, st);
-    return run_delta_dstate<DK, 2, 1>(a, st);
+  if constexpr (DK == 256) {
+    return tiles <= 256 ? run_delta_dstate<DK, 1, 4>(a, st) : run_delta_dstate<DK, 2, 2>(a, st);
   } else {
-    if (tiles <= 256) return run_delta_dstate<DK, 1, 4>(a, st);
-    if (DK == 256 || tiles <= 512) return run_delta_dstate<DK, 2, 2>(a, st);
-    if constexpr (DK == 128) return run_delta_dstate<DK, 4, 1>(a, st);
-    return hipErrorInvalidValue;
+    if (tiles > 1024 && a.dv % 128 == 0) return run_delta_dstate<DK, 8, 1>(a, st);
+    if (tiles > 512) return run_delta_dstate<DK, 4, 1>(a, st);
+    if constexpr (DK == 64) return run_delta_dstate<DK, 2, 1>(a, st);
+    else return tiles <= 256 ? run_delta_dstate<DK, 1, 4>(a, st) : run_delta_dstate<DK, 2, 2>(a, st);
   }
 }
 template <typename T>

@@ -36,7 +36,9 @@ namespace ccq {
 // sequential state pass needs no exponentials.
 // Blocks of 16: the diagonal blocks are inverted by forward substitution,
 // then wave w forms column block w, X_iw = -D_i sum_{m=w}^{i-1} A_im X_mw.
-template <typename T, int DK>
+// PLAIN (the delta rule without the contraction): shared query/key heads, and with
+// bf16 io the tail of Tm beside its head.
+template <typename T, int DK, bool PLAIN>
 __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   constexpr int C = kChunk;
   constexpr int P = Pad<T>::value;
@@ -50,7 +52,8 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   float* const sA = reinterpret_cast<float*>(sKAX);
   float* const sX = sA + C * LDA;
   __shared__ __align__(16) float sY[4][16 * 17];
-  __shared__ __align__(16) float sGam[C], sGamLo[C], sBeta[C];
+  __shared__ __align__(16) float sGam[C], sBeta[C];
+  __shared__ __align__(16) float sGamLo[PLAIN ? C : 4];  // what the rounding of gamma left
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
@@ -66,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
   // all global loads first (K, the log decays and beta), one round trip
   RowTile<T, DK> rk;
   RowScales<RowTile<T, DK>> fk;  // raw keys: row scales (l2 normalisation)
-  const KeyHead kh = key_head(a.HK, a.H, h);
+  const KeyHead kh = PLAIN ? key_head(a.HK, a.H, h) : KeyHead{a.H, h};
   rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
   if (a.rk) fk.load(a.rk + seq_idx(sq, r0, h, a.H), (size_t)a.H, nrow);
   float la = 0.f, bt = 0.f, rkt = 1.f;
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     const size_t ti = seq_idx(sq, r0 + (tid < nrow ? tid : nrow - 1), h, a.H);
     la = a.logalpha[ti];
     // a reset: e^-104 is already 0 in fp32, and the sums stay finite where it is -inf
-    if (a.HK && la < -104.f) la = -104.f;
+    if (PLAIN && la < -104.f) la = -104.f;
     bt = a.beta[ti];
     if (a.rk) rkt = a.rk[ti];
   }
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     float toC;  // gamma_C - gamma_j
     bt = tid < nrow ? bt : 0.f;
     float gC;
-    if (a.HK) {
+    if constexpr (PLAIN) {
       // the plain rule's final state is good to fp32: after resets |gamma| is large
       // against the differences that the decays are formed from, so they are taken
       // of 64-bit sums (a head and a tail in fp32)
@@ -108,7 +111,6 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
       }
       gC = __shfl(x, C - 1);
       toC = gC - x;
-      sGamLo[tid] = 0.f;
     }
     sGam[tid] = x;
     sBeta[tid] = bt;
@@ -146,12 +148,18 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     // select discards it
     const f32x4 gi = *reinterpret_cast<const f32x4*>(sGam + 16 * I + 4 * g4);
     const f32x4 bi = *reinterpret_cast<const f32x4*>(sBeta + 16 * I + 4 * g4);
-    const f32x4 gil = *reinterpret_cast<const f32x4*>(sGamLo + 16 * I + 4 * g4);
-    const float gj = sGam[16 * J + c16], gjl = sGamLo[16 * J + c16];
+    const float gj = sGam[16 * J + c16];
+    f32x4 gil = zero4();
+    float gjl = 0.f;
+    if constexpr (PLAIN) {
+      gil = *reinterpret_cast<const f32x4*>(sGamLo + 16 * I + 4 * g4);
+      gjl = sGamLo[16 * J + c16];
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * I + 4 * g4 + r, j = 16 * J + c16;
-      const float v = bi[r] * __expf((gi[r] - gj) + (gil[r] - gjl)) * acc[s3][r];
+      const float dg = PLAIN ? (gi[r] - gj) + (gil[r] - gjl) : gi[r] - gj;
+      const float v = bi[r] * __expf(dg) * acc[s3][r];
       sA[i * LDA + j] = j < i ? v : 0.f;
     }
   }
@@ -201,7 +209,7 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
     if ((lc >> 4) > (i >> 4)) lo = zero4();  // above the diagonal blocks
     if (((lc + 16) >> 4) > (i >> 4)) hi = zero4();
     store_acc_pair(Tout + i * C + 8 * q, lo, hi);
-    if (a.TmLo) {  // what the rounding of Tm left
+    if constexpr (PLAIN && sizeof(T) == 2) {  // what the rounding of Tm left
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         lo[e] -= f32(to<T>(lo[e]));
@@ -450,11 +458,13 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
 // of ld_frag_tr_acc_pair), so the update unpacks, accumulates and repacks in
 // place.
 //
-// PAIR (the plain rule, bf16): the scores enter the product with U as a bf16 head
+// PLAIN (the delta rule without the contraction): q is the caller's, of shared
+// query/key heads.  PAIR (that with bf16 io): the scores enter the product with U as a bf16 head
 // and tail, one rounding fewer in o (2.5e-3 instead of 3.0e-3 from the exact result
 // at the 1.3B shape, a stored bf16 value's own rounding being 1.7e-3).
-template <typename T, int DK, int VPW, int IPW, bool CARRY, bool PAIR>
+template <typename T, int DK, int VPW, int IPW, bool CARRY, bool PLAIN>
 __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArgs a) {
+  constexpr bool PAIR = PLAIN && sizeof(T) == 2;
   constexpr int C = kChunk;
   constexpr int P = Pad<T>::value;
   constexpr int LDQ = DK + P, LDP = C + P;
@@ -483,9 +493,9 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id();
   const int g4 = l >> 4, c16 = l & 15;
   const int vg = w % NVG, ig = NIG == 1 ? 0 : w / NVG;  // (uniform: no lane-masked branch on the tile)
-  const KeyHead kh = key_head(a.HK, a.H, h);
+  const KeyHead kh = PLAIN ? key_head(a.HK, a.H, h) : KeyHead{a.H, h};
   const size_t gstride = (size_t)kh.H * DK;
-  const Seq sqq = a.HK ? sq : padded_rows(sq, b, a.T);  // q_clean: the workspace's padded rows
+  const Seq sqq = PLAIN ? sq : padded_rows(sq, b, a.T);  // q_clean: the workspace's padded rows
   T* o = static_cast<T*>(a.o);
 
   Frag<T> sfr[VPW][NK];
@@ -654,7 +664,8 @@ hipError_t run_tri(const TriArgs& a, hipStream_t st) {
   const int N = (a.T + kChunk - 1) / kChunk;
   const int nblk = a.B * a.H * N;
   if (nblk == 0) return hipSuccess;
-  hipLaunchKernelGGL((gdn_tri_kernel<T, DK>), dim3(nblk), dim3(kThreads), 0, st, a);
+  if (a.HK) hipLaunchKernelGGL((gdn_tri_kernel<T, DK, true>), dim3(nblk), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((gdn_tri_kernel<T, DK, false>), dim3(nblk), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 template <typename T, int DK, int NPR, int NH>
@@ -684,8 +695,8 @@ hipError_t run_gdn_out_v(const GdnOutArgs& a, hipStream_t st) {
   const int N = (a.T + kChunk - 1) / kChunk;
   const int nblk = a.B * a.H * ((N + a.group - 1) / a.group);
   if (nblk == 0) return hipSuccess;
-  if (a.HK && sizeof(T) == 2)
-    hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry, sizeof(T) == 2>), dim3(nblk), dim3(kOutThreads), 0, st, a);
+  if (a.HK)
+    hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry, true>), dim3(nblk), dim3(kOutThreads), 0, st, a);
   else
     hipLaunchKernelGGL((gdn_out_kernel<T, DK, VPW, IPW, kCarry, false>), dim3(nblk), dim3(kOutThreads), 0, st, a);
   return hipGetLastError();
