@@ -276,10 +276,11 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * that several value heads share: value head h reads q and k of head h / (HV / HK).
  *   q, k [B,T,HK,dk], v, o [B,T,HV,dv] io_dtype; logalpha, beta [B,T,HV] fp32;
  *   S0, ST [B,HV,dv,dk] fp32 or NULL (zero; not wanted).
- * ST is as exact as fp32 arithmetic makes it whatever io_dtype is (bf16 operands
- * of the state's products are taken as head and tail), so the state may be handed
- * from segment to segment and to ccq_delta_step without a loss.  o and the
- * gradients carry bf16 products where io_dtype is bf16.
+ * ST keeps 17 bits of every operand whatever io_dtype is (with bf16 io, the operands
+ * of the state's products are taken as a bf16 head and tail: about 4e-6 from the
+ * exact state), so the state may be handed from segment to segment and to
+ * ccq_delta_step.  o and the gradients carry bf16 products where io_dtype is bf16
+ * (2.5e-3 to 3.5e-3).  logalpha below -104, -infinity included, is a reset (alpha = 0).
  * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
  * cu_seqlens of B + 1 int32, s->T a bound on the lengths; rows behind cu[B] (and
  * behind a sequence's first T) are not written.
@@ -371,7 +372,7 @@ ccq_status ccq_conv_bwd_varlen(const ccq_conv_shape* s, const int32_t* cu_seqlen
                                float* dbias, void* dstate0, void* workspace, size_t ws_bytes,
                                void* stream);
 /* One token per sequence (s->T must be 1): x, y [B,C] (x with pitch ldx); state
- * [B,W-1,C] io_dtype, moved on by the token in place. */
+ * [B,W-1,C] io_dtype, moved on by the token in place; x, y and state may not overlap. */
 ccq_status ccq_conv_step(const ccq_conv_shape* s, const void* x, const float* w, const float* bias,
                          void* state, void* y, void* stream);
 
@@ -402,6 +403,7 @@ typedef struct {
   int64_t ldx, ldg;
 } ccq_norm_shape;
 
+/* y may not overlap x or gate. */
 ccq_status ccq_norm_fwd(const ccq_norm_shape* s, const void* x, const float* w, const float* bias,
                         const void* gate, void* y, void* stream);
 /* Gradients: dy [rows,G,D] io_dtype, dense; dx, dgate [rows,G,D] io_dtype, dense (dgate with

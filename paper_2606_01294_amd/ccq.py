@@ -1027,6 +1027,9 @@ def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=Non
     _check(w, "w", (C, W), torch.float32, dev)
     _check(bias, "bias", (C,), torch.float32, dev)
     _check(state, "state", (B, W - 1, C), dt, dev)
+    (x0, x1), (s0, s1) = _span(x), _span(state)
+    if x0 < s1 and s0 < x1:
+        raise ValueError("state: shares memory with x")
     if out is None:
         y = torch.empty((B, C), dtype=dt, device=dev)
     else:
