@@ -367,7 +367,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
 
   __shared__ __align__(16) T sQ[C * LDQ];  // qc rows (kept to the end; read transposed there)
   __shared__ __align__(16) T sK[C * LDQ];
-  __shared__ float sGam[C], sBeta[C], sDec[C];
+  __shared__ __align__(16) float sGam[C], sBeta[C], sDec[C];
   __shared__ float sColF[4][C], sColA[4][C], sRV[C];
   __shared__ float sDg[C];
   __shared__ float sRed[2][NW];
@@ -426,6 +426,13 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   }
 
   // ---- phase 2: value slices
+  // fragment of U (token tile J, values k0 .. k0 + 31) by transposing reads of the
+  // U^T tile: a lane's four columns are four consecutive tokens in acc_pos order
+  constexpr int LDU = C + P;
+  auto u_frag = [&](const T* ut, int J, int k0) {
+    if constexpr (kFragD) return frag_tr_at(ut + k0 * LDU + frag_tr_pair_lane_off<T>(l, LDU) + 32 * (J >> 1) + 4 * (J & 1), LDU);
+    else return Frag<T>{};
+  };
   f32x4 G1[NTW], G2[NTW], G3[NTW], dP[NJ], dA[NJ];
 #pragma unroll
   for (int ct = 0; ct < NTW; ++ct) { G1[ct] = zero4(); G2[ct] = zero4(); G3[ct] = zero4(); }
@@ -439,7 +446,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   {
     T* sdO = reinterpret_cast<T*>(sR);
     T* sdR = sdO + C * LDV;
-    T* sU = sdR + C * LDV;
+    T* sU = sdR + C * LDV;  // rows = tokens (kFragD: U^T, rows v, tokens in acc_pos order)
     T* sV = sU + C * LDV;
     T* sS = sV + C * LDV;     // S_r slice, rows v (read transposed by the products)
     T* sD = sS + BV * LDQ;    // D slice, rows v
@@ -511,6 +518,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         *reinterpret_cast<v8*>(sS + vl * LDQ + 32 * m + 8 * pp) = cur.s[p];
         const int vd = kFragD ? vl : q / (DK / 8), cd = kFragD ? 32 * m + 8 * pp : (q % (DK / 8)) * 8;
         *reinterpret_cast<v8*>(sD + vd * LDQ + cd) = cur.d[p];
+        if constexpr (kFragD)  // <D, S_r>: the pieces hold the same elements
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dss += f32(cur.s[p][e]) * f32(cur.d[p][e]);
       }
 #pragma unroll
       for (int p = 0; p < NPU; ++p) {
@@ -519,8 +529,12 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
           const int vt = q / 128, rem = q % 128;
           const int m = rem / 64, vr = (rem % 64) / 4, pp = rem % 4;
           const int vl = 16 * vt + vr;
+          if constexpr (kFragD) {
+            *reinterpret_cast<v8*>(sU + vl * LDU + 32 * m + 8 * pp) = cur.u[p];
+          } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sU[(32 * m + acc_logical(8 * pp + e)) * LDV + vl] = cur.u[p][e];
+            for (int e = 0; e < 8; ++e) sU[(32 * m + acc_logical(8 * pp + e)) * LDV + vl] = cur.u[p][e];
+          }
         }
       }
       if (vv0 + BV < a.dv) load_slice(cur, vv0 + BV);
@@ -529,8 +543,17 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       for (int jj = 0; jj < NJ; ++jj) {
         const int J = HW * jj + hh;
         if (J <= sw) {
-          tile_mma<T, BV>(dP[jj], sdO + 16 * sw * LDV, LDV, sU + 16 * J * LDV, LDV);
-          tile_mma<T, BV>(dA[jj], sdR + 16 * sw * LDV, LDV, sU + 16 * J * LDV, LDV);
+          if constexpr (kFragD) {
+#pragma unroll
+            for (int k0 = 0; k0 < BV; k0 += 32) {
+              const Frag<T> fu = u_frag(sU, J, k0);
+              mma(dP[jj], ld_frag(sdO + 16 * sw * LDV + k0, LDV), fu);
+              mma(dA[jj], ld_frag(sdR + 16 * sw * LDV + k0, LDV), fu);
+            }
+          } else {
+            tile_mma<T, BV>(dP[jj], sdO + 16 * sw * LDV, LDV, sU + 16 * J * LDV, LDV);
+            tile_mma<T, BV>(dA[jj], sdR + 16 * sw * LDV, LDV, sU + 16 * J * LDV, LDV);
+          }
         }
       }
 #pragma unroll
@@ -540,10 +563,10 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
           const Frag<T> fs = ld_frag_tr(sS + k0 * LDQ + 16 * (ct0 + ct), LDQ);
           mma(G1[ct], ld_frag(sdO + 16 * sw * LDV + k0, LDV), fs);
           mma(G2[ct], ld_frag(sdR + 16 * sw * LDV + k0, LDV), fs);
-          mma(G3[ct], ld_frag(sU + 16 * sw * LDV + k0, LDV), ld_frag_tr(sD + k0 * LDQ + 16 * (ct0 + ct), LDQ));
+          mma(G3[ct], kFragD ? u_frag(sU, sw, k0) : ld_frag(sU + 16 * sw * LDV + k0, LDV), ld_frag_tr(sD + k0 * LDQ + 16 * (ct0 + ct), LDQ));
         }
       }
-      for (int idx = tid; idx < DK * BV / 8; idx += NT) {
+      for (int idx = tid; !kFragD && idx < DK * BV / 8; idx += NT) {
         const int vl = idx / (DK / 8), c = (idx % (DK / 8)) * 8;
         const v8 xs = *reinterpret_cast<const v8*>(sS + vl * LDQ + c);
         const v8 xd = *reinterpret_cast<const v8*>(sD + vl * LDQ + c);
@@ -595,10 +618,18 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       colF += F;
       colA += sBeta[i] * fa;
       sPm[i * LDT + j] = to<T>(pm);
-      sE[i * LDT + j] = to<T>(E);
       if constexpr (kPair) {
+        // E + E^T, zero on the diagonal: each entry below it goes to both places
+        const T eh = to<T>(E), el = to<T>(E - f32(eh));
         sPl[i * LDT + j] = to<T>(pm - f32(to<T>(pm)));
-        sEl[i * LDT + j] = to<T>(E - f32(to<T>(E)));
+        if (j <= i) {
+          sE[i * LDT + j] = eh;
+          sE[j * LDT + i] = eh;
+          sEl[i * LDT + j] = el;
+          sEl[j * LDT + i] = el;
+        }
+      } else {
+        sE[i * LDT + j] = to<T>(E);
       }
     }
     colF += __shfl_xor(colF, 16);
@@ -622,45 +653,125 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   float dot1[4] = {0.f, 0.f, 0.f, 0.f}, dot2[4] = {0.f, 0.f, 0.f, 0.f}, dot3[4] = {0.f, 0.f, 0.f, 0.f};
   float dl[4] = {0.f, 0.f, 0.f, 0.f};
   T* dqc_io = static_cast<T*>(a.dqc_io);
+  if constexpr (kPair) {
+    // dQ, then dK, each with its weights held as operands: x = Pm K, and y = Pm^T Q +
+    // (E + E^T) K
+    const bool own = a.HK == a.H;  // straight to the caller's rows, else fp32 to the workspace
+    // rows 16 sw + 4 g4 .. + 3 of channel c of dq or dk: neighbouring lanes swap two of
+    // their rows, so that each stores two channels of two
+    auto store = [&](const f32x4& v, int cc, void* io, float* wsp) {
+      typedef T v2 __attribute__((ext_vector_type(2)));
+      const bool odd = c16 & 1;
+      if (!own) {
 #pragma unroll
-  for (int ct = 0; ct < NTW; ++ct) {
-    f32x4 x = zero4(), y = zero4();
-    const int cc = 16 * (ct0 + ct);
-    tile_mma_bt<T, C>(x, sPm + 16 * sw * LDT, LDT, sK + cc, LDQ);
-    tile_mma_tr<T, C>(y, sPm + 16 * sw, LDT, sQ + cc, LDQ);
-    tile_mma_bt<T, C>(y, sE + 16 * sw * LDT, LDT, sK + cc, LDQ);
-    tile_mma_tr<T, C>(y, sE + 16 * sw, LDT, sK + cc, LDQ);
-    if constexpr (kPair) {
-      tile_mma_bt<T, C>(x, sPl + 16 * sw * LDT, LDT, sK + cc, LDQ);
-      tile_mma_tr<T, C>(y, sPl + 16 * sw, LDT, sQ + cc, LDQ);
-      tile_mma_bt<T, C>(y, sEl + 16 * sw * LDT, LDT, sK + cc, LDQ);
-      tile_mma_tr<T, C>(y, sEl + 16 * sw, LDT, sK + cc, LDQ);
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * sw + 4 * g4 + r;
+          if (i < nrow) wsp[rowoff + i * (int)gsk + cc + c16] = v[r];
+        }
+        return;
+      }
+      T* const out = static_cast<T*>(io) + seq_off(sq, r0, h, a.H, DK) + cc + (c16 & ~1);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float keep = odd ? v[2 + r] : v[r], got = lane_swap(odd ? v[r] : v[2 + r]);
+        const int i = 16 * sw + 4 * g4 + r + (odd ? 2 : 0);
+        if (i < nrow) *reinterpret_cast<v2*>(out + i * (int)gsk) = v2{to<T>(odd ? got : keep), to<T>(odd ? keep : got)};
+      }
+    };
+    f32x4 G;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) G[r] = __expf(sGam[16 * sw + 4 * g4 + r]);
+    {
+      Frag<T> wh[2], wl[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        wh[q] = ld_frag(sPm + 16 * sw * LDT + 32 * q, LDT);
+        wl[q] = ld_frag(sPl + 16 * sw * LDT + 32 * q, LDT);
+      }
+#pragma unroll
+      for (int ct = 0; ct < NTW; ++ct) {
+        const int cc = 16 * (ct0 + ct);
+        f32x4 x = zero4();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const Frag<T> kf = ld_frag_tr(sK + 32 * q * LDQ + cc, LDQ);
+          mma(x, wl[q], kf);
+          mma(x, wh[q], kf);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          dot1[r] += G1[ct][r] * f32(sQ[(16 * sw + 4 * g4 + r) * LDQ + cc + c16]);
+          x[r] += G[r] * G1[ct][r];
+        }
+        store(x, cc, a.dqc_io, a.dqc);
+      }
     }
-    const int c = cc + c16;
+    Frag<T> ph[2], pl[2], eh[2], el[2];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = 16 * sw + 4 * g4 + r;
-      const float G = __expf(sGam[i]);
-      const float qv = f32(sQ[i * LDQ + c]), kv = f32(sK[i * LDQ + c]);
-      const float dq = G * G1[ct][r] + x[r];
-      const float dk = y[r] + sDec[i] * G3[ct][r] - sBeta[i] * G * G2[ct][r];
-      dot1[r] += G1[ct][r] * qv;
-      dot2[r] += G2[ct][r] * kv;
-      dot3[r] += G3[ct][r] * kv;
-      if (PLAIN && i < nrow && a.HK == a.H) {
-        const size_t off = seq_off(sq, r0 + i, h, a.H, DK) + c;
-        dqc_io[off] = to<T>(dq);
-        static_cast<T*>(a.dk_io)[off] = to<T>(dk);
-      } else if (PLAIN && i < nrow) {
-        const size_t off = rowoff + i * (int)gsk + c;
-        a.dqc[off] = dq;
-        a.dk_bb[off] = dk;
-      } else if (!PLAIN && i < nrow) {
-        const size_t off = rowoff + i * (int)gsk + c;
-        a.dqc[off] = dq;
-        dqc_io[off] = to<T>(dq);
-        a.dk_bb[off] = dk;
-        dl[r] -= dq * cr[ct][r];
+    for (int q = 0; q < 2; ++q) {
+      ph[q] = ld_frag_tr(sPm + 32 * q * LDT + 16 * sw, LDT);
+      pl[q] = ld_frag_tr(sPl + 32 * q * LDT + 16 * sw, LDT);
+      eh[q] = ld_frag(sE + 16 * sw * LDT + 32 * q, LDT);
+      el[q] = ld_frag(sEl + 16 * sw * LDT + 32 * q, LDT);
+    }
+    const f32x4 dec = *reinterpret_cast<const f32x4*>(sDec + 16 * sw + 4 * g4);
+    const f32x4 bG = G * *reinterpret_cast<const f32x4*>(sBeta + 16 * sw + 4 * g4);
+#pragma unroll
+    for (int ct = 0; ct < NTW; ++ct) {
+      const int cc = 16 * (ct0 + ct);
+      f32x4 y = zero4();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const Frag<T> qf = ld_frag_tr(sQ + 32 * q * LDQ + cc, LDQ), kf = ld_frag_tr(sK + 32 * q * LDQ + cc, LDQ);
+        mma(y, pl[q], qf);
+        mma(y, el[q], kf);
+        mma(y, ph[q], qf);
+        mma(y, eh[q], kf);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float kv = f32(sK[(16 * sw + 4 * g4 + r) * LDQ + cc + c16]);
+        dot2[r] += G2[ct][r] * kv;
+        dot3[r] += G3[ct][r] * kv;
+        y[r] += dec[r] * G3[ct][r] - bG[r] * G2[ct][r];
+      }
+      store(y, cc, a.dk_io, a.dk_bb);
+    }
+  } else {
+#pragma unroll
+    for (int ct = 0; ct < NTW; ++ct) {
+      f32x4 x = zero4(), y = zero4();
+      const int cc = 16 * (ct0 + ct);
+      tile_mma_bt<T, C>(x, sPm + 16 * sw * LDT, LDT, sK + cc, LDQ);
+      tile_mma_tr<T, C>(y, sPm + 16 * sw, LDT, sQ + cc, LDQ);
+      tile_mma_bt<T, C>(y, sE + 16 * sw * LDT, LDT, sK + cc, LDQ);
+      tile_mma_tr<T, C>(y, sE + 16 * sw, LDT, sK + cc, LDQ);
+      const int c = cc + c16;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = 16 * sw + 4 * g4 + r;
+        const float G = __expf(sGam[i]);
+        const float qv = f32(sQ[i * LDQ + c]), kv = f32(sK[i * LDQ + c]);
+        const float dq = G * G1[ct][r] + x[r];
+        const float dk = y[r] + sDec[i] * G3[ct][r] - sBeta[i] * G * G2[ct][r];
+        dot1[r] += G1[ct][r] * qv;
+        dot2[r] += G2[ct][r] * kv;
+        dot3[r] += G3[ct][r] * kv;
+        if (PLAIN && i < nrow && a.HK == a.H) {
+          const size_t off = seq_off(sq, r0 + i, h, a.H, DK) + c;
+          dqc_io[off] = to<T>(dq);
+          static_cast<T*>(a.dk_io)[off] = to<T>(dk);
+        } else if (PLAIN && i < nrow) {
+          const size_t off = rowoff + i * (int)gsk + c;
+          a.dqc[off] = dq;
+          a.dk_bb[off] = dk;
+        } else if (!PLAIN && i < nrow) {
+          const size_t off = rowoff + i * (int)gsk + c;
+          a.dqc[off] = dq;
+          dqc_io[off] = to<T>(dq);
+          a.dk_bb[off] = dk;
+          dl[r] -= dq * cr[ct][r];
+        }
       }
     }
   }
