@@ -8,6 +8,7 @@
 
 #include "ccq_device.h"
 #include "ccq_kernels.h"
+#include "ccq_plain.h"
 
 namespace ccq {
 

@@ -706,15 +706,6 @@ __device__ __forceinline__ Seq padded_rows(const Seq& q, int b, int T) { return 
 __device__ __forceinline__ size_t seq_off(const Seq& q, int t, int h, int H, int D) {
   return ((size_t)(q.row0 + t) * H + h) * (size_t)D;
 }
-// Query/key heads of a tensor and the one that value head h (of H) reads: with HK
-// query/key heads, consecutive H / HK value heads share one; HK = 0: every value
-// head has its own.
-struct KeyHead {
-  int H, h;
-};
-__device__ __forceinline__ KeyHead key_head(int HK, int H, int h) {
-  return HK ? KeyHead{HK, h / (H / HK)} : KeyHead{H, h};
-}
 // Index of token t of sequence q, head h, in a [rows, H] tensor.
 __device__ __forceinline__ size_t seq_idx(const Seq& q, int t, int h, int H) {
   return (size_t)(q.row0 + t) * H + h;
@@ -730,11 +721,6 @@ __device__ __forceinline__ float group_sum(float x) {
   if constexpr (N >= 8) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x101F));
   if constexpr (N >= 16) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x201F));
   return x;
-}
-
-// The value of the neighbouring lane (lane ^ 1).
-__device__ __forceinline__ float lane_swap(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));
 }
 
 // Scalar per-token value prefetched by lane `row` (clamped address, zeroed at use).

@@ -28,6 +28,7 @@
 // (acc_pos) over the chunk's tokens.
 #include "ccq_device.h"
 #include "ccq_kernels.h"
+#include "ccq_plain.h"
 
 namespace ccq {
 
