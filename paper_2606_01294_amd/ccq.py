@@ -1027,14 +1027,15 @@ def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=Non
     _check(w, "w", (C, W), torch.float32, dev)
     _check(bias, "bias", (C,), torch.float32, dev)
     _check(state, "state", (B, W - 1, C), dt, dev)
-    (x0, x1), (s0, s1) = _span(x), _span(state)
-    if x0 < s1 and s0 < x1:
+    ld, size = _pitch(x, 1, "x"), x.element_size()
+    x0, s0 = x.data_ptr(), state.data_ptr()
+    if x0 < s0 + B * (W - 1) * C * size and s0 < x0 + B * ld * size:
         raise ValueError("state: shares memory with x")
     if out is None:
         y = torch.empty((B, C), dtype=dt, device=dev)
     else:
         y = _outputs({"y": out}, {"y": ((B, C), dt)}, dev, (x, w, bias, state))["y"]
-    shape = ConvShape(B, 1, C, W, _dt(dt), int(act), _pitch(x, 1, "x"))
+    shape = ConvShape(B, 1, C, W, _dt(dt), int(act), ld)
     _launch("ccq_conv_step", dev, stream, shape, (x, w, bias, state, y))
     if stream is not None:
         _record(stream, y)

@@ -192,3 +192,7 @@ def test_out_may_not_share_memory():
         ccq.ccq_conv_fwd(x, w.to(BF))
     with pytest.raises(ccq.CcqError):
         ccq.ccq_conv_fwd(x, torch.zeros(64, 5, device="cuda"))
+    st = torch.zeros(4, 3, 64, device="cuda", dtype=BF)
+    with pytest.raises(ValueError):
+        ccq.ccq_conv_step(st[:, 1], w, st)  # the token among the state that it moves on
+    assert ccq.ccq_conv_step(st[:, 1].clone(), w, st).shape == (4, 64)
