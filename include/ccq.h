@@ -283,7 +283,9 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * (2.5e-3 to 3.5e-3).  logalpha below -104, -infinity included, is a reset (alpha = 0).
  * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
  * cu_seqlens of B + 1 int32, s->T a bound on the lengths; rows behind cu[B] (and
- * behind a sequence's first T) are not written.
+ * behind a sequence's first T) are not written.  An infinity or NaN among a token's
+ * inputs reaches the outputs of its whole chunk of 64 tokens and of those behind it
+ * (ccq_delta_step: of the tokens behind it), never another sequence or head.
  * Supported: dv in {64,128,256,512}; dk in {64,128,256} (bf16 io) or {64,128} (fp32
  * io); the training step with fp32 io: dk = 64; ccq_delta_step: dk in {64,128,256},
  * both types.  B > 65535 packed is CCQ_ERR_UNSUPPORTED.
@@ -342,7 +344,7 @@ typedef enum { CCQ_ACT_NONE = 0, CCQ_ACT_SILU = 1, CCQ_ACT_SIGMOID = 2 } ccq_act
  *   io_dtype, dense.  state0 [B,W-1,C] io_dtype: the W - 1 inputs before the first
  *   token, oldest first (NULL: zeros); stateT the same after the last one (NULL: not
  *   wanted; may not overlap state0).
- * Supported: W in {2,3,4}, C a positive multiple of 8, ldx >= C with ldx elements a
+ * Supported: W in {2,3,4}, C a positive multiple of 8 up to 2^24, ldx >= C with ldx elements a
  * multiple of 16 bytes.  Packed batches: x, y [rows,C], offsets and T as above.
  */
 typedef struct {

@@ -355,13 +355,14 @@ hipError_t conv_dispatch(const ConvArgs& a, int W, ConvCall call, hipStream_t st
 }
 }  // namespace
 
-// Thread indices are 32 bits wide.
-bool conv_supported(int B, int T, int C, int W) {
-  if (W < 2 || W > 4 || C < 8 || C % 8) return false;
-  const long long runs = conv_runs(T, kConvRun);
-  return (long long)B * runs * (C / 4) < (1ll << 31) - kConvThreads;
-}
 long long conv_part_rows(int B, int T) { return (long long)B * ((conv_runs(T, kConvRunB) + 3) / 4); }
+// Thread indices, and the threads of a launch, are 32 bits wide.
+bool conv_supported(int B, int T, int C, int W) {
+  if (W < 2 || W > 4 || C < 8 || C % 8 || C > (1 << 24)) return false;
+  const long long runs = conv_runs(T, kConvRun), ncb = (C / kConvVeB + 63) / 64;
+  return (long long)B * runs * (C / 4) < (1ll << 31) - kConvThreads &&
+         conv_part_rows(B, T) * ncb < (1ll << 32) / kConvThreads;
+}
 
 hipError_t launch_conv(const ConvArgs& a, int W, ConvCall call, bool is_bf16, hipStream_t st) {
   return is_bf16 ? conv_dispatch<bf16_t>(a, W, call, st) : conv_dispatch<float>(a, W, call, st);

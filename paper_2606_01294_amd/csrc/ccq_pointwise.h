@@ -36,9 +36,10 @@ struct Act {
     // -z log2(e) - t, with log2(e) to 48 bits
     float r = __builtin_fmaf(-z, 1.44269504f, -t);
     r = __builtin_fmaf(-z, 1.92596303e-8f, r);
+    // (a t or e that overflows takes no correction: infinity times it is NaN)
     r = fabsf(t) < 1e30f ? r * 0.693147181f : 0.f;
     const float e = __builtin_amdgcn_exp2f(t);
-    const float d = 1.f + __builtin_fmaf(e, r, e);
+    const float d = 1.f + (e < 3e38f ? __builtin_fmaf(e, r, e) : e);
     const float q = __builtin_amdgcn_rcpf(d);
     return d < 3e38f ? __builtin_fmaf(__builtin_fmaf(-d, q, 1.f), q, q) : q;
   }

@@ -196,3 +196,66 @@ def test_out_may_not_share_memory():
     with pytest.raises(ValueError):
         ccq.ccq_conv_step(st[:, 1], w, st)  # the token among the state that it moves on
     assert ccq.ccq_conv_step(st[:, 1].clone(), w, st).shape == (4, 64)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+def test_activations_far_from_zero(act, dt):
+    """z from 0 to where e^-z overflows, beyond, and infinite: values and derivatives are those of
+    the formula (less what is below the smallest normal number), and NaN only where it has one."""
+    inf = float("inf")
+    z = torch.tensor([0.0, 1e-3, 1, 20, 60, 80, 87, 87.5, 88, 88.5, 88.7, 89, 90, 95, 100, 103.5, 104,
+                      110, 128, 150, 200, 1e3, 1e6, 1e20, 1e30, 3e38, inf, 2, 3, 4, 5, 6])
+    z = torch.cat([z, -z]).to(dt)
+    C = 8
+    x = z[:, None, None].expand(-1, 1, C).contiguous().cuda()  # one token a sequence: z = 1 x
+    w = torch.zeros(C, 2, device="cuda")
+    w[:, 1] = 1
+    leaf = z.double().requires_grad_()
+    ref = act64(act, leaf)
+    finite = torch.isfinite(z)
+    slope, = torch.autograd.grad(ref[finite].sum(), leaf)
+    ref = ref.detach()
+    y = ccq.ccq_conv_fwd(x, w, act=ACTS[act])["y"][:, 0].double().cpu()
+    state = torch.zeros(len(z), 1, C, dtype=dt, device="cuda")
+    step = ccq.ccq_conv_step(x[:, 0].contiguous(), w, state, act=ACTS[act]).double().cpu()
+    dx = ccq.ccq_conv_bwd(x, w, torch.ones_like(x), act=ACTS[act])["dx"][:, 0].double().cpu()
+    half = {BF: 2.0 ** -8, F32: 2.0 ** -24}[dt]
+    work = {BF: 2.0 ** -16, F32: 64 * 2.0 ** -24}[dt]
+    for got in (y, step):
+        r = ref[:, None].expand_as(got)
+        assert torch.equal(torch.isnan(got), torch.isnan(r))
+        assert torch.equal(torch.isinf(got), torch.isinf(r))
+        m = torch.isfinite(r)
+        assert bool(((got - r)[m].abs() <= (half + work) * r[m].abs()
+                     + 2.0 ** -126 * z.double().abs().clamp(1, 128)[:, None].expand_as(r)[m]).all())
+    r = slope[finite][:, None].expand(-1, C)
+    # silu' = s (1 + z (1 - s)): its terms are up to 1 + |z| s, and 1 - s is held to 2^-24
+    zf = z[finite].double()
+    size = torch.sigmoid(zf) * (1 + zf.abs().clamp(max=128)) + 2.0 ** -100
+    assert bool(((dx[finite] - r).abs() <= half * r.abs() + work * size[:, None]).all())
+
+
+def test_poison_reaches_its_window_alone():
+    """A NaN reaches its channel's next W - 1 outputs and no other sequence or channel."""
+    lens, C, W = [70, 40, 33], 16, 4
+    x, w, b, s0, dy, dsT = make(lens, C, W, F32, True, True)
+    cu = torch.tensor([0, 70, 110, 143], dtype=torch.int32).cuda()
+    d = [t.cuda() for t in (x, w, b, s0, dy, dsT)]
+    fwd = lambda x: ccq.ccq_conv_fwd_varlen(x, d[1], cu, 70, d[2], d[3])["y"]  # noqa: E731
+    bwd = lambda x: ccq.ccq_conv_bwd_varlen(x, d[1], d[4], cu, 70, d[2], d[3], d[5])  # noqa: E731
+    bad = d[0].clone()
+    bad[30, 5] = float("nan")   # a run's boundary follows at 32
+    bad[109, 7] = float("nan")  # the second sequence's last token
+    hit = torch.zeros(143, C, dtype=torch.bool, device="cuda")
+    hit[30:34, 5] = True
+    hit[109, 7] = True
+    y0, y1 = fwd(d[0]), fwd(bad)
+    assert torch.equal(torch.isnan(y1), hit) and torch.equal(y0[~hit], y1[~hit])
+    g0, g1 = bwd(d[0]), bwd(bad)
+    hit[27:30, 5] = True
+    hit[106:109, 7] = True
+    assert torch.equal(torch.isnan(g1["dx"]), hit) and torch.equal(g0["dx"][~hit], g1["dx"][~hit])
+    rest = [c for c in range(C) if c not in (5, 7)]
+    assert torch.equal(g0["dw"][rest], g1["dw"][rest])
+    assert torch.equal(g0["dstate0"], g1["dstate0"])

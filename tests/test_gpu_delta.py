@@ -235,3 +235,38 @@ def test_refusals():
         ccq.ccq_delta_fwd(q, k, v, la, be, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         ccq.ccq_delta_step(q, k, v, la, be, None)
+
+
+@pytest.mark.parametrize("dk,dv,dt", [(128, 256, BF), (256, 256, BF), (64, 64, F32), (64, 128, BF)])
+@pytest.mark.parametrize("poison", [float("nan"), float("inf")])
+def test_poison_stays_in_its_sequence(dk, dv, dt, poison):
+    """Infinities and NaN in one sequence, in the rows behind the last one, and in another value
+    head change no bit of the others' results; ahead of a poisoned token's chunk o is as it was."""
+    lens, HK, HV = [70, 33, 130, 5], 2, 4
+    d = make(lens, HK, HV, dk, dv, dt, True)
+    n = sum(lens)
+    cu = torch.tensor([0] + [sum(lens[:i + 1]) for i in range(len(lens))], dtype=torch.int32).cuda()
+    clean = {m: torch.cat([t, torch.zeros(7, *t.shape[1:], dtype=t.dtype)])
+             for m, t in d.items() if m != "S"}
+    dirty = {m: t.clone() for m, t in clean.items()}
+    for t in dirty.values():
+        t[70:103] = poison
+        t[n:] = poison
+    S0 = d["S"].cuda()
+    kw = dict(S0=S0, want_states=True)
+    call = lambda t: ccq.ccq_delta_fwd_bwd_varlen(*dev(t), t["dO"].cuda(), cu, max(lens), **kw)  # noqa: E731
+    want, got = call(clean), call(dirty)
+    for m in want:
+        a, b = (want[m], got[m]) if m == "ST" else (want[m][:n], got[m][:n])
+        keep = [0, 2, 3] if m == "ST" else list(range(70)) + list(range(103, n))
+        assert torch.equal(a[keep], b[keep]), m
+    # a value head of the third sequence, from its token 64 on
+    dirty = {m: t.clone() for m, t in clean.items()}
+    dirty["v"][103 + 64, 1, 3] = poison
+    got = call(dirty)
+    heads = [0, 2, 3]
+    for m in ("o", "dv", "dlogalpha", "dbeta"):
+        assert torch.equal(want[m][:n, heads], got[m][:n, heads]), m
+    assert torch.equal(want["ST"][:, heads], got["ST"][:, heads])
+    assert torch.equal(want["o"][:103 + 64], got["o"][:103 + 64])
+    assert not bool(torch.isfinite(got["o"][103 + 64, 1]).all())
