@@ -34,13 +34,20 @@ namespace ccq {
 namespace {
 constexpr int kNormThreads = 256;
 
-// Sum over the LPI lanes (or, for LPI = 256, the workgroup) that hold an item.
+// x + the value of the lane that CTRL names within the row of 16.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// Sum over the LPI lanes (or, for LPI = 256, the workgroup) that hold an item: the
+// first four steps within the vector unit (a row of 16 lanes), where a step costs a
+// few cycles instead of a trip through the LDS crossbar.
 template <int LPI>
 __device__ __forceinline__ float item_sum(float x, float* red) {
-  if constexpr (LPI >= 2) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x041F));
-  if constexpr (LPI >= 4) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x081F));
-  if constexpr (LPI >= 8) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x101F));
-  if constexpr (LPI >= 16) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x201F));
+  if constexpr (LPI >= 2) x = dpp_add<0xB1>(x);    // lane ^ 1
+  if constexpr (LPI >= 4) x = dpp_add<0x4E>(x);    // lane ^ 2
+  if constexpr (LPI >= 8) x = dpp_add<0x141>(x);   // mirrored in 8: the other four
+  if constexpr (LPI >= 16) x = dpp_add<0x140>(x);  // mirrored in 16: the other eight
   if constexpr (LPI >= 32) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x401F));
   if constexpr (LPI >= 64) x += __shfl_xor(x, 32);
   if constexpr (LPI > 64) {  // four waves; the array is free again after the second barrier
@@ -162,8 +169,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_kernel(const NormArgs a
 template <typename T, int LPI, int NV, bool GATE>
 __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a) {
   typedef Vec8<T> V;
-  constexpr int SPW = LPI < 64 ? 64 / LPI : 1;  // slots per wave
-  constexpr int SPB = kNormThreads / LPI;       // per workgroup
+  constexpr int SPB = kNormThreads / LPI;  // slots per workgroup
   __shared__ float red[4];
   const ItemCols<LPI, NV> ic{(int)(threadIdx.x % LPI), a.D / 8};
   const unsigned rb = blockIdx.x / a.G;
@@ -251,29 +257,34 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(const NormArgs a
   const bool bias = a.bias != nullptr;
   const size_t cols = (size_t)(a.shared ? 1 : a.G) * a.D;  // of dw
   const size_t pitch = cols * (bias ? 2 : 1);
-  __shared__ float buf[LPI > 64 ? 1 : 4][LPI > 64 ? 1 : LPI * NV * 8];
+  // every slot's sums to LDS, then a column's over the slots in order
+  __shared__ __align__(16) float buf[2][LPI > 64 ? 1 : SPB][LPI > 64 ? 4 : LPI * NV * 8];
   float* out = a.part + (a.shared ? (size_t)blockIdx.x * pitch : (size_t)rb * pitch + (size_t)head * a.D);
-  for (int q = 0; q < (bias ? 2 : 1); ++q) {
 #pragma unroll
-    for (int u = 0; u < NV; ++u)
+  for (int u = 0; u < NV; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float t = q ? db[u][e] : dw[u][e];
-        if constexpr (SPW > 1)
-#pragma unroll
-          for (int off = LPI; off < 64; off <<= 1) t += __shfl_xor(t, off);
-        if constexpr (LPI > 64) {
-          if (ic.has(u)) out[q * cols + ic.col(u) + e] = t;
-        } else if (lane_id() < LPI) {
-          buf[wave_id()][ic.j * 8 + LPI * 8 * u + e] = t;
+    for (int e = 0; e < 8; e += 4) {
+      const f32x4 w4 = {dw[u][e], dw[u][e + 1], dw[u][e + 2], dw[u][e + 3]};
+      const f32x4 b4 = {db[u][e], db[u][e + 1], db[u][e + 2], db[u][e + 3]};
+      if constexpr (LPI > 64) {
+        if (ic.has(u)) {
+          *reinterpret_cast<f32x4*>(out + ic.col(u) + e) = w4;
+          if (bias) *reinterpret_cast<f32x4*>(out + cols + ic.col(u) + e) = b4;
         }
+      } else {
+        *reinterpret_cast<f32x4*>(&buf[0][threadIdx.x / LPI][ic.col(u) + e]) = w4;
+        if (bias) *reinterpret_cast<f32x4*>(&buf[1][threadIdx.x / LPI][ic.col(u) + e]) = b4;
       }
-    if constexpr (LPI <= 64) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < a.D; i += kNormThreads)
-        out[q * cols + i] = (buf[0][i] + buf[1][i]) + (buf[2][i] + buf[3][i]);
-      __syncthreads();
     }
+  if constexpr (LPI <= 64) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.D; i += kNormThreads)
+      for (int q = 0; q < (bias ? 2 : 1); ++q) {
+        float t[4] = {};
+#pragma unroll
+        for (int k = 0; k < SPB; ++k) t[k % 4] += buf[q][k][i];
+        out[q * cols + i] = (t[0] + t[1]) + (t[2] + t[3]);
+      }
   }
 }
 
@@ -292,12 +303,15 @@ long long norm_slots(long long rows, int G, int lanes) {
   if (step < 1) step = 1;
   return (rows < step ? rows : step) * G;
 }
-// Backward: row blocks of SPB rows at a time for each head, 4 workgroups a compute
-// unit in all (what its registers admit).
+// Backward: row blocks of SPB rows at a time for each head, at most 4 workgroups a
+// compute unit in all (what its registers admit), and no more than make every block
+// take as many turns (4099 rows of 5 heads of 96, fp32: 129 blocks of two turns 14 us,
+// 205 of one or two 16).
 long long norm_row_blocks(long long rows, int G, int lanes) {
   const long long spb = kNormThreads / lanes;
   const long long most = (1024 + G - 1) / G, need = (rows + spb - 1) / spb;
-  return most < need ? most : need;
+  const long long turns = need > 0 ? (need + most - 1) / most : 1;
+  return (need + turns - 1) / turns;
 }
 template <typename T, int LPI, int NV>
 hipError_t run_norm(const NormArgs& a, bool bwd, hipStream_t st) {
