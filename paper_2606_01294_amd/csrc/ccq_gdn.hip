@@ -248,6 +248,8 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
   __shared__ __align__(16) T sV[2][C * LDV];
   __shared__ __align__(16) float sCf[2][4][C];  // beta e^gamma, beta, e^{gamma_C - gamma}, e^{gamma_C}
   __shared__ __align__(16) f32x4 sX[NH > 1 ? NW * 4 * 64 : 1];  // partial P of every wave
+  constexpr bool kShareU = sizeof(T) == 4 && (NH == 2 || NH == 4);
+  __shared__ __align__(16) f32x4 sU[kShareU ? NPR * 4 * 64 : 1];  // U's tiles
 
   const int nvt = a.dv / BVS;
   const int N = (a.T + C - 1) / C;
@@ -387,15 +389,32 @@ __global__ __launch_bounds__(64 * NPR * NH, 1) void gdn_state_kernel(const GdnAr
         for (int r = 0; r < 4; ++r) R[J][r] = bj[r] * frag_elem(vf, 4 * hh + r) - bg[r] * R[J][r];
       }
     }
-    // U = Tm R (Tm rows are stored in acc_pos order)
+    // U = Tm R (Tm rows are stored in acc_pos order; right of the diagonal tiles it is
+    // zero).  In fp32 the products are long enough to share the row tiles out over
+    // the waves of a slice: a long one with a short one
     const Frag<T> rf0 = acc_pair_frag<T>(R[0], R[1]);
     const Frag<T> rf1 = acc_pair_frag<T>(R[2], R[3]);
     f32x4 U[4];
+    auto u_tile = [&](int I) {
+      f32x4 u = zero4();
+      mma(u, ld_frag(sT[buf] + 16 * I * LDT, LDT), rf0);
+      if (I >= 2) mma(u, ld_frag(sT[buf] + 16 * I * LDT + 32, LDT), rf1);
+      return u;
+    };
+    if constexpr (kShareU) {
+      f32x4* const su = sU + (size_t)pr * 4 * 64 + l;
+      if constexpr (NH == 2) {
+        su[64 * hq] = u_tile(hq);
+        su[64 * (3 - hq)] = u_tile(3 - hq);
+      } else {
+        su[64 * hq] = u_tile(hq);
+      }
+      lds_barrier();
 #pragma unroll
-    for (int I = 0; I < 4; ++I) {
-      U[I] = zero4();
-      mma(U[I], ld_frag(sT[buf] + 16 * I * LDT, LDT), rf0);
-      mma(U[I], ld_frag(sT[buf] + 16 * I * LDT + 32, LDT), rf1);
+      for (int I = 0; I < 4; ++I) U[I] = su[64 * I];
+    } else {
+#pragma unroll
+      for (int I = 0; I < 4; ++I) U[I] = u_tile(I);
     }
     // U^T (kept for the write-back), then U e^{gamma_C - gamma_i}
     uf[0] = acc_pair_frag<T>(U[0], U[1]);
