@@ -683,15 +683,18 @@ def _on_gpu(t, name):
 
 
 def _outputs(out, want, dev, inputs):
-    """The outputs named in `want` (name -> (shape, dtype)), from `out` where given."""
-    if not out:
-        return {n: torch.empty(shp, dtype=dt, device=dev) for n, (shp, dt) in want.items()}
+    """The outputs named in `want` (name -> (shape, dtype), or a dense tensor like it), from `out`
+    where given."""
+    if not out:  # (torch makes a tensor like another in 0.8 us, one of a named shape in 1.4)
+        return {n: torch.empty_like(w) if isinstance(w, torch.Tensor) else
+                torch.empty(w[0], dtype=w[1], device=dev) for n, w in want.items()}
     extra = set(out) - set(want)
     if extra:
         raise ValueError("out: no output named %s here" % ", ".join(sorted(extra)))
     spans = [_span(t) for t in inputs if t is not None]
     res = {}
-    for n, (shp, dt) in want.items():
+    for n, w in want.items():
+        shp, dt = (w.shape, w.dtype) if isinstance(w, torch.Tensor) else w
         t = out.get(n)
         if t is None:
             t = torch.empty(shp, dtype=dt, device=dev)
@@ -824,7 +827,7 @@ def _delta_fwd(q, k, v, logalpha, beta, cu_seqlens, max_len, S0, scale, want_sta
     dev = q.device
     state = (shape.B, shape.HV, shape.dv, shape.dk)
     _check(S0, "S0", state, torch.float32, dev)
-    want = {"o": (tuple(v.shape), q.dtype)}
+    want = {"o": v}
     if want_states:
         want["ST"] = (state, torch.float32)
     res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0))
@@ -863,10 +866,9 @@ def _delta_fwd_bwd(q, k, v, logalpha, beta, dO, cu_seqlens, max_len, S0, scale, 
     _check(S0, "S0", state, torch.float32, dev)
     _check(dO, "dO", v.shape, dt, dev)
     gates = tok + (shape.HV,)
-    want = {"dq": (tuple(q.shape), dt), "dk": (tuple(q.shape), dt), "dv": (tuple(v.shape), dt),
-            "dlogalpha": (gates, dt), "dbeta": (gates, dt)}
+    want = {"dq": q, "dk": q, "dv": v, "dlogalpha": (gates, dt), "dbeta": (gates, dt)}
     if want_o:
-        want["o"] = (tuple(v.shape), dt)
+        want["o"] = v
     if want_states:
         want["ST"] = (state, torch.float32)
     res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0, dO))
@@ -914,10 +916,9 @@ def ccq_delta_step(q, k, v, logalpha, beta, S, scale=1.0, out=None, stream=None)
                             (beta, "beta", (B, T, HV), f32), (S, "S", (B, HV, dv, dk), f32)):
         _check(t, name, shp, d, dev)
     if out is None:
-        o = torch.empty((B, T, HV, dv), dtype=dt, device=dev)
+        o = torch.empty_like(v)
     else:
-        o = _outputs({"o": out}, {"o": ((B, T, HV, dv), dt)}, dev,
-                     (q, k, v, logalpha, beta, S))["o"]
+        o = _outputs({"o": out}, {"o": v}, dev, (q, k, v, logalpha, beta, S))["o"]
     shape = DeltaShape(B, T, HK, HV, dk, dv, _dt(dt), scale)
     _launch("ccq_delta_step", dev, stream, shape, (q, k, v, logalpha, beta, S, o))
     if stream is not None:
@@ -948,7 +949,7 @@ def _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act):
 def _conv_fwd(x, w, cu_seqlens, max_len, bias, state0, act, want_state, out, stream):
     shape = _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act)
     dev = x.device
-    want = {"y": (tuple(x.shape), x.dtype)}
+    want = {"y": x if x.is_contiguous() else (tuple(x.shape), x.dtype)}
     if want_state:
         want["stateT"] = ((shape.B, shape.W - 1, shape.C), x.dtype)
     res = _outputs(out, want, dev, (x, w, bias, state0))
@@ -978,15 +979,15 @@ def ccq_conv_fwd_varlen(x, w, cu_seqlens, max_len, bias=None, state0=None, act=C
 
 def _conv_bwd(x, w, dy, cu_seqlens, max_len, bias, state0, dstateT, act, out, workspace, stream):
     shape = _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act)
-    dev, dt, f32 = x.device, x.dtype, torch.float32
+    dev, dt = x.device, x.dtype
     state = (shape.B, shape.W - 1, shape.C)
     _check(dy, "dy", x.shape, dt, dev)
     _check(dstateT, "dstateT", state, dt, dev)
-    want = {"dx": (tuple(x.shape), dt), "dw": (tuple(w.shape), f32)}
+    want = {"dx": dy, "dw": w}
     if bias is not None:
-        want["dbias"] = (tuple(bias.shape), f32)
+        want["dbias"] = bias
     if state0 is not None:
-        want["dstate0"] = (state, dt)
+        want["dstate0"] = state0
     res = _outputs(out, want, dev, (x, w, bias, state0, dy, dstateT))
     ws = _scratch(workspace, int(lib().ccq_conv_workspace_size(shape)), dev)
     args = [x, w, bias, state0, dy, dstateT, res["dx"], res["dw"], res.get("dbias"),
@@ -1027,12 +1028,13 @@ def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=Non
     _check(w, "w", (C, W), torch.float32, dev)
     _check(bias, "bias", (C,), torch.float32, dev)
     _check(state, "state", (B, W - 1, C), dt, dev)
-    ld, size = _pitch(x, 1, "x"), x.element_size()
+    dense = x.is_contiguous()
+    ld, size = C if dense else _pitch(x, 1, "x"), x.element_size()
     x0, s0 = x.data_ptr(), state.data_ptr()
     if x0 < s0 + B * (W - 1) * C * size and s0 < x0 + B * ld * size:
         raise ValueError("state: shares memory with x")
     if out is None:
-        y = torch.empty((B, C), dtype=dt, device=dev)
+        y = torch.empty_like(x) if dense else torch.empty((B, C), dtype=dt, device=dev)
     else:
         y = _outputs({"y": out}, {"y": ((B, C), dt)}, dev, (x, w, bias, state))["y"]
     shape = ConvShape(B, 1, C, W, _dt(dt), int(act), ld)
@@ -1055,13 +1057,15 @@ def _norm_shape(x, weight, bias, gate, kind, act, eps):
     wshape = (D,) if shared else (G, D)
     _check(weight, "weight", wshape, torch.float32, dev)
     _check(bias, "bias", wshape, torch.float32, dev)
-    ldg = G * D
+    ldx = ldg = G * D
     if gate is not None:
         if gate.shape != x.shape or gate.dtype != dt or gate.device != dev:
             _check(gate, "gate", x.shape, dt, dev)
-        ldg = _pitch(gate, 2, "gate")
-    return NormShape(rows, G, D, _dt(dt), int(kind), int(act), int(shared), float(eps),
-                     _pitch(x, 2, "x"), ldg)
+        if not gate.is_contiguous():
+            ldg = _pitch(gate, 2, "gate")
+    if not x.is_contiguous():
+        ldx = _pitch(x, 2, "x")
+    return NormShape(rows, G, D, _dt(dt), int(kind), int(act), int(shared), float(eps), ldx, ldg)
 
 
 def ccq_norm_fwd(x, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, act=CCQ_ACT_SILU,
@@ -1073,7 +1077,7 @@ def ccq_norm_fwd(x, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, act=CC
     shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
     dev = x.device
     if out is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        y = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=dev)
     else:
         y = _outputs({"y": out}, {"y": (tuple(x.shape), x.dtype)}, dev, (x, weight, bias, gate))["y"]
     _launch("ccq_norm_fwd", dev, stream, shape, (x, weight, bias, gate, y))
@@ -1086,15 +1090,15 @@ def ccq_norm_bwd(x, dy, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, ac
                  eps=1e-5, out=None, workspace=None, stream=None):
     """Gradients of ccq_norm_fwd for dy [..., G, D].  Returns dict dx[, dweight][, dbias][, dgate]."""
     shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
-    dev, dt, f32 = x.device, x.dtype, torch.float32
+    dev, dt = x.device, x.dtype
     _check(dy, "dy", x.shape, dt, dev)
-    want = {"dx": (tuple(x.shape), dt)}
+    want = {"dx": dy}
     if weight is not None:
-        want["dweight"] = (tuple(weight.shape), f32)
+        want["dweight"] = weight
     if bias is not None:
-        want["dbias"] = (tuple(bias.shape), f32)
+        want["dbias"] = bias
     if gate is not None:
-        want["dgate"] = (tuple(x.shape), dt)
+        want["dgate"] = dy
     res = _outputs(out, want, dev, (x, dy, weight, bias, gate))
     need = int(lib().ccq_norm_workspace_size(shape)) if weight is not None else 0
     ws = _scratch(workspace, need, dev)
