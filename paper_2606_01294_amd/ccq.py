@@ -981,6 +981,8 @@ def _conv_bwd(x, w, dy, cu_seqlens, max_len, bias, state0, dstateT, act, out, wo
     shape = _conv_shape(x, w, bias, state0, cu_seqlens, max_len, act)
     dev, dt = x.device, x.dtype
     state = (shape.B, shape.W - 1, shape.C)
+    if dy is None:
+        raise ValueError("dy is required")
     _check(dy, "dy", x.shape, dt, dev)
     _check(dstateT, "dstateT", state, dt, dev)
     want = {"dx": dy, "dw": w}
@@ -1091,6 +1093,8 @@ def ccq_norm_bwd(x, dy, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, ac
     """Gradients of ccq_norm_fwd for dy [..., G, D].  Returns dict dx[, dweight][, dbias][, dgate]."""
     shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
     dev, dt = x.device, x.dtype
+    if dy is None:
+        raise ValueError("dy is required")
     _check(dy, "dy", x.shape, dt, dev)
     want = {"dx": dy}
     if weight is not None:

@@ -37,7 +37,7 @@ namespace ccq {
 // chunk ahead, into two.  A loader has one chunk in flight at most, so it waits for
 // all of its loads and counts none.
 //
-// 1.3B forward (B = 4, T = 4096, H = 8, dk = dv = 256): 170 us, 5700 cycles a chunk: 1300
+// 1.3B forward (B = 4, T = 4096, H = 8, dk = dv = 256): 170 to 187 us, 5700 cycles a chunk: 1300
 // of them products, 3300 of LDS traffic (334 KB a chunk and compute unit: K rows and
 // transposed, Tm twice, the exchange), the rest the latency of the chain K S -> sum ->
 // R -> Tm R -> update.  One wave a tile takes 167 to 178 us there, features split over
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 // two bytes a lane and row, dR held them up.  Operands are bf16, D and every sum fp32 (D and dR
 // are rounded as operands and on store).
 // 1.3B training step (B = 4, T = 4096, H = 8, dk = dv = 256): 335 us in the form of
-// gdn_dstate_kernel, which stages through registers, 225 in this one.
+// gdn_dstate_kernel, which stages through registers, 235 to 240 in this one.
 template <int DK, int NPR, int NH>
 struct DeltaBackTile {
   static constexpr int C = kChunk, NLW = 4, BVS = 16 * NPR, NC = NPR * NH;

@@ -23,8 +23,9 @@
 // Sums, statistics and the affine part are fp32; what is stored is rounded once.
 //
 // 16,384 tokens of 8 heads of 256, bf16, gated: forward 43 us (201 MB, 4.6 TB/s; a copy
-// of that size from memory runs at 5.1), backward 66 us (335 MB, 5.1 TB/s) and 5 us
-// for the partial rows.
+// of that size from memory runs at 5.1), backward 65 us (335 MB, 5.1 TB/s) and 5 us
+// for the partial rows; 4099 rows of 5 heads of 96, fp32: 10 and 4 us, launches and the
+// latency of two turns.
 #include "ccq_device.h"
 #include "ccq_kernels.h"
 #include "ccq_pointwise.h"
