@@ -270,3 +270,28 @@ def test_poison_stays_in_its_sequence(dk, dv, dt, poison):
     assert torch.equal(want["ST"][:, heads], got["ST"][:, heads])
     assert torch.equal(want["o"][:103 + 64], got["o"][:103 + 64])
     assert not bool(torch.isfinite(got["o"][103 + 64, 1]).all())
+
+
+@pytest.mark.parametrize("HK,HV", [(1, 1), (1, 2)])
+def test_gradient_against_differences(HK, HV):
+    """fp32 io, four points along a direction that holds the gradient itself.  o is off by 1e-6 of
+    its norm, which 18 / 12 over a step of 2^-6 makes 2^-13 of |dO| |o|; the fifth derivative
+    along a step of a fiftieth of the inputs adds less than 2^-10 of the slope."""
+    T, h = 66, 2.0 ** -6
+    d = make([T], HK, HV, 64, 64, F32, True)
+    args, dO, S0 = dev(d, (1, T)), d["dO"].cuda().view(1, T, HV, 64), d["S"].cuda()
+    got = ccq.ccq_delta_fwd_bwd(*args, dO, S0=S0)
+
+    def loss(i, x):
+        o = ccq.ccq_delta_fwd(*[x if j == i else a for j, a in enumerate(args)], S0=S0)["o"]
+        return float((o.double() * dO.double()).sum())
+    size = float(dO.norm() * got["o"].norm())
+    for i, n in enumerate(("dq", "dk", "dv", "dlogalpha", "dbeta")):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        v = got[n] / got[n].square().mean().sqrt() + torch.randn(args[i].shape, generator=g, device="cuda")
+        v = v * (0.125 if i < 2 else 0.5 if i > 2 else 1.0)  # a q or k element is 2^-3, a beta 2^-1
+        at = {k: loss(i, args[i] + k * h * v) for k in (-2, -1, 1, 2)}
+        num = (8 * (at[1] - at[-1]) - (at[2] - at[-2])) / (12 * h)
+        ana = float((got[n].double() * v.double()).sum())
+        print(n, num, ana, flush=True)
+        assert abs(num - ana) <= 2.0 ** -13 * size + 2.0 ** -10 * abs(ana), n

@@ -159,3 +159,33 @@ def test_refusals():
         ccq.ccq_norm_fwd(x, bias=w)
     with pytest.raises(ccq.CcqError):
         ccq.ccq_norm_fwd(x[..., :60].contiguous())
+
+
+def slope(loss, args, i, v, h=2.0 ** -6):
+    """Derivative of the loss along v in args[i] from four points (off by h^4 / 30 of the fifth)."""
+    def at(k):
+        return loss(*[a + k * h * v if j == i else a for j, a in enumerate(args)])
+    return (8 * (at(1) - at(-1)) - (at(2) - at(-2))) / (12 * h)
+
+
+@pytest.mark.parametrize("kind,gated,act", [("group", False, "silu"), ("rms", True, "silu"),
+                                            ("l2", True, "sigmoid"), ("group", True, "none")])
+def test_gradient_against_differences(kind, gated, act):
+    """fp32 io.  Every y is off by 2^-18 at most (the tolerance above, a quarter of it a step's
+    difference), which 18 / 12 over 2^-6 makes 2^-12 of the sum of |dy|; the fifth derivative along
+    a step of a hundredth of the inputs adds less than 2^-10 of the slope."""
+    x, w, b, gate, dy = [t if t is None else t.cuda() for t in
+                         make((3,), 2, 40, F32, kind, "bias", True, gated)]
+    args = [x, w, b] + ([gate] if gated else [])
+    kw = dict(kind=KINDS[kind], act=ACTS[act])
+    got = ccq.ccq_norm_bwd(x, dy, weight=w, bias=b, gate=gate, **kw)
+
+    def loss(x, w, b, gate=None):
+        y = ccq.ccq_norm_fwd(x, weight=w, bias=b, gate=gate, **kw)
+        return float((y.double() * dy.double()).sum())
+    for i, n in enumerate(("dx", "dweight", "dbias", "dgate")[:len(args)]):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        v = got[n] / got[n].square().mean().sqrt() + torch.randn(args[i].shape, generator=g, device="cuda")
+        num, ana = slope(loss, args, i, v), float((got[n].double() * v.double()).sum())
+        print(n, num, ana, flush=True)
+        assert abs(num - ana) <= 2.0 ** -12 * float(dy.abs().sum()) + 2.0 ** -10 * abs(ana), n
