@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libccq.so")
 SOURCES = ["ccq_clean.hip", "ccq_gla.hip", "ccq_gdn.hip", "ccq_gdn_roles.hip", "ccq_bwd.hip", "ccq_gdn_bwd.hip", "ccq_decode.hip", "ccq_prep.hip", "ccq_util.hip",
-           "ccq_delta.hip", "ccq_norm.hip", "ccq_conv.hip", "ccq_api.cpp", "ccq_layer_api.cpp"]
+           "ccq_delta.hip", "ccq_delta_short.hip", "ccq_norm.hip", "ccq_conv.hip", "ccq_api.cpp", "ccq_layer_api.cpp"]
 ARCH = "gfx950"
 
 # Packed fp32 vector ops are switched off for all device code (-packed-fp32-ops).

@@ -313,6 +313,29 @@ struct HeadSumArgs {
   const int* cu = nullptr;
 };
 
+// Gradients for a few tokens, token by token (bf16 io): hist [B,HV,T,dv,dk], part
+// [B,HV,T,dv/4,2,dk] and gpart [B,HV,T,dv/4,2] are workspace.
+struct DeltaShortArgs {
+  const void* q;          // [B,T,HK,dk] (or packed rows) io
+  const void* k;          // [B,T,HK,dk] io
+  const void* v;          // [B,T,HV,dv] io
+  const void* dO;         // [B,T,HV,dv] io
+  const float* logalpha;  // [B,T,HV]
+  const float* beta;      // [B,T,HV]
+  const float* S0;        // [B,HV,dv,dk] fp32 or null
+  float* hist;
+  float* part;
+  float* gpart;
+  void* dq_out;           // [B,T,HK,dk] io
+  void* dk_out;           // [B,T,HK,dk] io
+  void* dv_out;           // [B,T,HV,dv] io
+  void* dla_io;           // [B,T,HV] io
+  void* dbeta_io;         // [B,T,HV] io
+  int B, T, HK, HV, dk, dv;
+  float scale;
+  const int* cu = nullptr;
+};
+
 // ---- recurrent decode (one token per sequence, cache updated in place) ----
 struct DecodeArgs {
   const void* q;         // [B,H,dk] io
@@ -457,6 +480,12 @@ hipError_t launch_delta_state(const GdnArgs& a, hipStream_t st);         // bf16
 hipError_t launch_delta_dstate(const GdnDstateArgs& a, hipStream_t st);  // bf16
 hipError_t launch_delta_step(const DeltaStepArgs& a, bool is_bf16, hipStream_t st);
 hipError_t launch_head_sum(const HeadSumArgs& a, bool is_bf16, hipStream_t st);
+bool delta_short(int B, int T, int HV, bool is_bf16);
+size_t delta_short_hist(int B, int T, int HV, int dk, int dv);
+size_t delta_short_part(int B, int T, int HV, int dk, int dv);
+size_t delta_short_gpart(int B, int T, int HV, int dv);
+hipError_t launch_delta_short(const DeltaShortArgs& a, hipStream_t st);
+hipError_t launch_delta_short_sum(const DeltaShortArgs& a, hipStream_t st);
 hipError_t launch_copy_or_zero(float* dst, const float* src, size_t n, hipStream_t st);
 
 hipError_t launch_gla_dstate(const DstateArgs& a, bool is_bf16, bool gate_bf16, hipStream_t st);

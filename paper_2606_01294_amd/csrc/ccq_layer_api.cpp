@@ -37,6 +37,7 @@ ccq_status check_delta(const ccq_delta_shape* s, bool bwd) {
 struct DeltaLayout {
   size_t states = 0, Tm = 0, TmLo = 0, gam = 0, U = 0;          // forward
   size_t PT = 0, TmT = 0, dstates = 0, dR = 0, dq = 0, dk = 0;  // training step
+  size_t hist = 0, part = 0, gpart = 0;                         // the same, a few tokens
   size_t total = 0;
 };
 DeltaLayout delta_layout(const ccq_delta_shape* s, bool bwd) {
@@ -50,7 +51,11 @@ DeltaLayout delta_layout(const ccq_delta_shape* s, bool bwd) {
   if (s->io_dtype == CCQ_BF16) L.TmLo = take(nchunk * 64 * 64 * e);
   L.gam = take(nchunk * 5 * 64 * sizeof(float));
   L.U = take(nchunk * 64 * s->dv * e);
-  if (bwd) {
+  if (bwd && ccq::delta_short(s->B, s->T, s->HV, s->io_dtype == CCQ_BF16)) {
+    L.hist = take(ccq::delta_short_hist(s->B, s->T, s->HV, s->dk, s->dv) * sizeof(float));
+    L.part = take(ccq::delta_short_part(s->B, s->T, s->HV, s->dk, s->dv) * sizeof(float));
+    L.gpart = take(ccq::delta_short_gpart(s->B, s->T, s->HV, s->dv) * sizeof(float));
+  } else if (bwd) {
     L.PT = take(nchunk * 64 * 64 * e);
     L.TmT = take(nchunk * 64 * 64 * e);
     L.dstates = take(nchunk * s->dv * s->dk * e);
@@ -102,6 +107,18 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
   const int B = s->B, T = s->T, H = s->HV;
   float* gam = reinterpret_cast<float*>(ws + L.gam);
   trace_begin_call();
+  // a few tokens: the gradients token by token, the chunked form where o or ST is wanted
+  const bool few = g && ccq::delta_short(B, T, H, bf);
+  if (few) {
+    float* const f[] = {reinterpret_cast<float*>(ws + L.hist), reinterpret_cast<float*>(ws + L.part),
+                        reinterpret_cast<float*>(ws + L.gpart)};
+    ccq::DeltaShortArgs da{q, k, v, g->dO, la, beta, S0, f[0], f[1], f[2], g->dq, g->dk, g->dv, g->dla, g->dbeta,
+                           B, T, s->HK, H, s->dk, s->dv, s->scale, cu};
+    if (traced(st, [&] { return ccq::launch_delta_short(da, st); }) != hipSuccess) return CCQ_ERR_HIP;
+    if (traced(st, [&] { return ccq::launch_delta_short_sum(da, st); }) != hipSuccess) return CCQ_ERR_HIP;
+    if (!o && !ST) return CCQ_OK;
+    g = nullptr;
+  }
   // chunk transforms and decay coefficients, then the chain of chunk states
   ccq::TriArgs ta{k, la, beta, ws + L.Tm, gam, B, T, H, s->dk, s->dv};
   ta.cu = cu;

@@ -35,20 +35,10 @@ namespace ccq {
 namespace {
 constexpr int kNormThreads = 256;
 
-// x + the value of the lane that CTRL names within the row of 16.
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-// Sum over the LPI lanes (or, for LPI = 256, the workgroup) that hold an item: the
-// first four steps within the vector unit (a row of 16 lanes), where a step costs a
-// few cycles instead of a trip through the LDS crossbar.
+// Sum over the LPI lanes (or, for LPI = 256, the workgroup) that hold an item.
 template <int LPI>
 __device__ __forceinline__ float item_sum(float x, float* red) {
-  if constexpr (LPI >= 2) x = dpp_add<0xB1>(x);    // lane ^ 1
-  if constexpr (LPI >= 4) x = dpp_add<0x4E>(x);    // lane ^ 2
-  if constexpr (LPI >= 8) x = dpp_add<0x141>(x);   // mirrored in 8: the other four
-  if constexpr (LPI >= 16) x = dpp_add<0x140>(x);  // mirrored in 16: the other eight
+  x = row_sum<LPI < 16 ? LPI : 16>(x);
   if constexpr (LPI >= 32) x += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x401F));
   if constexpr (LPI >= 64) x += __shfl_xor(x, 32);
   if constexpr (LPI > 64) {  // four waves; the array is free again after the second barrier

@@ -1,6 +1,5 @@
-// ccq_pointwise.h -- device helpers of the memory-bound operators around the
-// recurrence (convolution, norm): vectors of channels, activations, and sums of
-// the rows of a matrix of partial sums.
+// ccq_pointwise.h -- device helpers of the operators around the recurrence: vectors of
+// channels, sums over lanes, activations.
 #pragma once
 #include "ccq_device.h"
 #include "ccq_kernels.h"
@@ -21,6 +20,22 @@ struct VecN {
   }
 };
 template <typename T> using Vec8 = VecN<T, 8>;
+
+// x + the value of the lane that CTRL names within the row of 16.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// Sum over aligned groups of N <= 16 lanes within the vector unit, where a step costs a
+// few cycles instead of a trip through the LDS crossbar.
+template <int N>
+__device__ __forceinline__ float row_sum(float x) {
+  if constexpr (N >= 2) x = dpp_add<0xB1>(x);    // lane ^ 1
+  if constexpr (N >= 4) x = dpp_add<0x4E>(x);    // lane ^ 2
+  if constexpr (N >= 8) x = dpp_add<0x141>(x);   // mirrored in 8: the other four
+  if constexpr (N >= 16) x = dpp_add<0x140>(x);  // mirrored in 16: the other eight
+  return x;
+}
 
 // act(z) and act'(z): none, silu (z sigmoid z), sigmoid.  bf16 io takes the
 // hardware's exponential and reciprocal as they are (about 1e-6 relative, far

@@ -295,3 +295,44 @@ def test_gradient_against_differences(HK, HV):
         ana = float((got[n].double() * v.double()).sum())
         print(n, num, ana, flush=True)
         assert abs(num - ana) <= 2.0 ** -13 * size + 2.0 ** -10 * abs(ana), n
+
+
+@pytest.mark.parametrize("lens,HK,HV,dk,dv,state,gates", [
+    ([1], 1, 1, 64, 64, False, "mild"), ([1], 1, 1, 256, 256, True, "mild"),
+    ([1, 1, 1], 2, 6, 128, 64, True, "resets"), ([2], 1, 1, 128, 128, False, "mild"),
+    ([3, 3], 1, 2, 64, 512, True, "strong"), ([17], 1, 3, 128, 256, True, "mild"),
+    ([16] * 4, 2, 2, 64, 128, False, "still"), ([64], 1, 2, 256, 64, True, "mild"),
+    ([7, 0, 1, 9, 2], 1, 2, 128, 128, True, "resets"), ([0, 3], 2, 2, 256, 256, False, "mild")])
+def test_gradients_of_a_few_tokens(lens, HK, HV, dk, dv, state, gates):
+    """Up to 64 tokens (128 times value heads) the gradients are formed in fp32: half a step of bf16 and
+    the sums' own work, a few 2^-22 of their terms, each at most a row of dO against a row of v
+    (or of the state, or of both): 2^-18 of the norms' product."""
+    d = make(lens, HK, HV, dk, dv, BF, state, gates)
+    ref = solve(d, lens, 0.7, True)
+    n = sum(lens)
+    work = 2.0 ** -18 * float(d["dO"].double().norm(dim=-1).max()) * (
+        1 + float(d["v"].double().norm(dim=-1).max()) + (float(d["S"].double().norm(dim=(-2, -1)).max()) if state else 0))
+    kw = dict(S0=d["S"].cuda() if state else None, scale=0.7)
+    names = ("dq", "dk", "dv", "dlogalpha", "dbeta")
+
+    def held(got):
+        for m in names:
+            a, r = got[m].double().cpu().reshape(ref[m].shape), ref[m]
+            off = (a - r).abs() - 2.0 ** -8 * r.abs()
+            print(m, float(off.max()) if n else 0, work, flush=True)
+            assert bool((off <= work * (HV // HK)).all()), m
+    cu = torch.tensor([0] + [sum(lens[:i + 1]) for i in range(len(lens))], dtype=torch.int32).cuda()
+    wide = {m: torch.cat([t, torch.full((4, *t.shape[1:]), float("nan"), dtype=t.dtype)])
+            for m, t in d.items() if m != "S"}
+    out = {m: torch.full((n + 4, *ref[m].shape[1:]), 3.0, dtype=BF, device="cuda") for m in names}
+    ccq.ccq_delta_fwd_bwd_varlen(*dev(wide), wide["dO"].cuda(), cu, max(lens), out=out, want_o=False, **kw)
+    assert all(bool((out[m][n:] == 3.0).all()) for m in names)
+    held({m: t[:n] for m, t in out.items()})
+    if len(set(lens)) == 1:
+        B, T = len(lens), lens[0]
+        got = ccq.ccq_delta_fwd_bwd(*dev(d, (B, T)), d["dO"].cuda().view(B, T, HV, dv), want_states=True, **kw)
+        held(got)
+        assert all(torch.equal(got[m].view_as(out[m][:n]), out[m][:n]) for m in names)
+        check(got, ref, TOL[BF], ("o", "ST"))
+        fwd = ccq.ccq_delta_fwd(*dev(d, (B, T)), **kw)
+        assert torch.equal(fwd["o"], got["o"]) and torch.equal(fwd["ST"], got["ST"])
