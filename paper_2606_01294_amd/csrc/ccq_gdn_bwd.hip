@@ -48,7 +48,8 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int bh = lb / N, ci = lb % N;
+  const ChunkOf id = a.HK && a.cu ? chunk_of(blockIdx.x, a.B, a.HK, a.H, N) : ChunkOf{lb / N, lb % N};
+  const int bh = id.bh, ci = id.ci;
   const int b = bh / a.H, h = bh % a.H;
   const Seq sq = seq_of(a.cu, b, a.T), sp = padded_rows(sq, b, a.T);
   const int r0 = ci * C;
@@ -384,7 +385,8 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int bh = lb / N, ci = lb % N;
+  const ChunkOf id = PLAIN && a.cu ? chunk_of(blockIdx.x, a.B, a.HK, a.H, N) : ChunkOf{lb / N, lb % N};
+  const int bh = id.bh, ci = id.ci;
   const int b = bh / a.H, h = bh % a.H;
   const Seq sq = seq_of(a.cu, b, a.T), sp = padded_rows(sq, b, a.T);
   const int r0 = ci * C;
