@@ -280,8 +280,8 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * of the state's products are taken as a bf16 head and tail: about 4e-6 from the
  * exact state), so the state may be handed from segment to segment and to
  * ccq_delta_step.  o and the gradients carry bf16 products where io_dtype is bf16
- * (2.5e-3 to 3.5e-3; gradients of up to 64 tokens, 128 times value heads, are formed
- * in fp32, as a gate's would be of chance there).  logalpha below -104, -infinity included, is a reset (alpha = 0).
+ * (2.5e-3 to 3.5e-3); with T <= 64 and B T HV <= 128 the gradients are formed in fp32,
+ * since a norm over so few numbers does not average the products' errors out.  logalpha below -104, -infinity included, is a reset (alpha = 0).
  * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
  * cu_seqlens of B + 1 int32, s->T a bound on the lengths; rows behind cu[B] (and
  * behind a sequence's first T) are not written.  An infinity or NaN among a token's

@@ -3,7 +3,7 @@
 //
 // The chunked form is that of ccq_gdn.hip (transforms Tm, state pass, outputs),
 // read with the caller's queries; value head h reads query/key head h / (HV / HK).
-// Its backward is that of ccq_gdn_bwd.hip.
+// Its backward is that of ccq_gdn_bwd.hip (of a few tokens, ccq_delta_short.hip).
 #include <type_traits>
 
 #include "ccq_device.h"
