@@ -185,11 +185,12 @@ __global__ __launch_bounds__(kThreadsS) void delta_short_sum_kernel(const DeltaS
 }
 
 // Up to 64 tokens a sequence (of the bound on the lengths), 128 tokens times value heads:
-// there the chunked form's norms do not average its errors out (at 64 x 1 up to 4.9e-3
-// over 24 draws, 2.1e-3 here; beyond, 130 x 1, 4.1e-3 at most), and its seven launches
-// cost as much (whole calls with o, 64 x 64 and 256 x 256: 27 and 30 us for one token here;
-// 64 tokens of 2 heads 59 and 90, the chunked form 39 and 61; 16 of 8 heads 32 and 75,
-// chunked 35 and 55).
+// there the chunked form's norms do not average its errors out (64 x 1: up to 4.9e-3 over
+// 24 draws, 2.1e-3 here; beyond, with 130 to 136 numbers, 4.7e-3 at most over 64 draws at
+// each of eight lengths, 4e-3 for nine in ten), and its seven launches cost as much
+// (whole calls with o, 64 x 64 and 256 x 256: 27 and 30 us for one token here; 64 tokens
+// of 2 heads 59 and 90, the chunked form 39 and 61; 16 of 8 heads 32 and 75, chunked 35
+// and 55).
 bool delta_short(int B, int T, int HV, bool is_bf16) {
   return is_bf16 && T <= kShortLen && (long long)B * T * HV <= 128;
 }
