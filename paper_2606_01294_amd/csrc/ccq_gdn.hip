@@ -104,7 +104,9 @@ __global__ __launch_bounds__(kThreads) void gdn_tri_kernel(const TriArgs a) {
       x = (float)xd;
       toC = (float)(gd - xd);
       gC = (float)gd;
-      sGamLo[tid] = (float)(xd - (double)x);
+      const float tail = (float)(xd - (double)x);
+      sGamLo[tid] = tail;
+      a.gamLo[((size_t)bh * N + ci) * C + tid] = tail;  // for the kernels that form decays from gamma
     } else {
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
@@ -499,6 +501,7 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
   __shared__ __align__(16) T sP[C * LDP];  // P[i][acc_pos(j)]
   __shared__ __align__(16) T sPl[PAIR ? C * LDP : 1];  // what its rounding left
   __shared__ __align__(16) float sGam[C];
+  __shared__ float sGamLo[PLAIN ? C : 1];  // what the rounding of gamma left
   __shared__ __align__(16) float sDd[C + 4];  // e^{gamma_C - gamma_j}; e^{gamma_C} at C
   __shared__ float sRk[C];                    // raw keys: row scales of the scores
 
@@ -530,6 +533,7 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
       rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), gstride, nrow);
       const float* gm = a.gam + ((size_t)bh * N + ci) * 5 * C;
       if (tid < C) sGam[tid] = gm[tid];
+      if (PLAIN && tid < C) sGamLo[tid] = a.gamLo[((size_t)bh * N + ci) * C + tid];
       if (a.rk && tid < C) sRk[tid] = a.rk[seq_idx(sq, r0 + (tid < nrow ? tid : nrow - 1), h, a.H)];
       if (carry && tid < C + 1) sDd[tid] = tid < C ? gm[3 * C + tid] : gm[4 * C];
       rq.store(sQ, LDQ);
@@ -572,7 +576,9 @@ __global__ __launch_bounds__(kOutThreads, 1) void gdn_out_kernel(const GdnOutArg
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int j = 16 * J + 4 * g4 + r;
-          x[r] = j <= i ? sc[r] * __expf(gi - sGam[j]) * (a.rk ? sRk[j] : 1.f) : 0.f;
+          float dg = gi - sGam[j];
+          if constexpr (PLAIN) dg += sGamLo[i] - sGamLo[j];
+          x[r] = j <= i ? sc[r] * __expf(dg) * (a.rk ? sRk[j] : 1.f) : 0.f;
         }
       }
       store4(sP + i * LDP + acc_pos(16 * J + 4 * g4), x[0], x[1], x[2], x[3]);

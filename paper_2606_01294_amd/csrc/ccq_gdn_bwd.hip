@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
   __shared__ __align__(16) T sQ[C * LDQ];
   __shared__ __align__(16) T sK[C * LDQ];
   __shared__ __align__(16) T sTm[C * LDP];
-  __shared__ float sGam[C];
+  __shared__ float sGam[C], sGamLo[C];  // gamma, and (the plain rule) what its rounding left
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
@@ -65,7 +65,10 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
     rq.load(static_cast<const T*>(a.qc) + seq_off(a.HK ? sq : sp, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     rt.load(static_cast<const T*>(a.Tm) + cidx * C * C, (size_t)C, C);
-    if (tid < C) sGam[tid] = a.gam[cidx * 5 * C + tid];
+    if (tid < C) {
+      sGam[tid] = a.gam[cidx * 5 * C + tid];
+      sGamLo[tid] = a.gamLo ? a.gamLo[cidx * C + tid] : 0.f;
+    }
     rq.store(sQ, LDQ);
     rk.store(sK, LDQ);
     rt.store(sTm, LDP);
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * I + 4 * g4 + r;
-      x[r] = (t < 10 && j <= i) ? acc[r] * __expf(sGam[i] - sGam[j]) : 0.f;
+      x[r] = (t < 10 && j <= i) ? acc[r] * __expf((sGam[i] - sGam[j]) + (sGamLo[i] - sGamLo[j])) : 0.f;
     }
     store4(PT + (size_t)j * C + 16 * I + 4 * g4, x[0], x[1], x[2], x[3]);
   }
@@ -370,6 +373,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
   __shared__ __align__(16) T sQ[C * LDQ];  // qc rows (kept to the end; read transposed there)
   __shared__ __align__(16) T sK[C * LDQ];
   __shared__ __align__(16) float sGam[C], sBeta[C], sDec[C];
+  __shared__ float sGamLo[PLAIN ? C : 1];  // what the rounding of gamma left
   __shared__ float sColF[4][C], sColA[4][C], sRV[C];
   __shared__ float sDg[C];
   __shared__ float sRed[2][NW];
@@ -410,6 +414,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
     rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), gsq, nrow);
     if (tid < C) {
       sGam[tid] = a.gam[cidx * 5 * C + tid];
+      if constexpr (PLAIN) sGamLo[tid] = a.gamLo[cidx * C + tid];
       sBeta[tid] = a.gam[(cidx * 5 + 2) * C + tid];
       sDec[tid] = a.gam[(cidx * 5 + 3) * C + tid];
     }
@@ -610,7 +615,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * sw + 4 * g4 + r;
-      const float e = (J <= sw && j <= i) ? __expf(sGam[i] - sGam[j]) : 0.f;
+      float dg = sGam[i] - sGam[j];
+      if constexpr (PLAIN) dg += sGamLo[i] - sGamLo[j];
+      const float e = (J <= sw && j <= i) ? __expf(dg) : 0.f;
       const float pm = e * dP[jj][r];
       const float ea = j < i ? -e * dA[jj][r] : 0.f;  // (M o dA)_ij
       const float E = sBeta[i] * ea;

@@ -137,6 +137,7 @@ struct TriArgs {
   // and the tail of Tm (Tm is then the head of a bf16 pair), or null
   int HK = 0;
   void* TmLo = nullptr;
+  float* gamLo = nullptr;  // [B*H, N, C]: what the rounding of gamma to fp32 left (written), or null
 };
 
 // Gated DeltaNet state recurrence (sequential over chunks): writes the
@@ -176,6 +177,7 @@ struct GdnOutArgs {
   const int* cu = nullptr;  // as TriArgs
   const float* rk = nullptr;  // key row scales (the scores'; the carry's come with the coefficients)
   int HK = 0;  // as TriArgs; if set, qc holds the caller's queries (its rows, HK heads)
+  const float* gamLo = nullptr;  // as TriArgs (with HK)
 };
 
 // ---- training step (CCQ-GLA backward) ----
@@ -242,6 +244,7 @@ struct GdnPrepArgs {
   int B, T, H, dk, dv;
   const int* cu = nullptr;  // packed-batch offsets (device), as CleanArgs
   int HK = 0;               // as GdnOutArgs
+  const float* gamLo = nullptr;  // as GdnOutArgs
 };
 
 // Reverse scan of the state adjoint D = dS_{r+1} over the chunks of one head:
@@ -285,6 +288,7 @@ struct GdnBwdArgs {
   // with HK = H dq and dk to the caller's rows in io dtype (dqc_io, dk_io), else
   // every value head's in fp32 to the workspace (dqc, dk_bb); no corr, no dlam
   int HK = 0;
+  const float* gamLo = nullptr;  // as GdnOutArgs
   void* dk_io = nullptr;
   void* dla_io = nullptr;
   void* dbeta_io = nullptr;

@@ -35,7 +35,7 @@ ccq_status check_delta(const ccq_delta_shape* s, bool bwd) {
 }
 
 struct DeltaLayout {
-  size_t states = 0, Tm = 0, TmLo = 0, gam = 0, U = 0;          // forward
+  size_t states = 0, Tm = 0, TmLo = 0, gam = 0, gamLo = 0, U = 0;  // forward
   size_t PT = 0, TmT = 0, dstates = 0, dR = 0, dq = 0, dk = 0;  // training step
   size_t hist = 0, part = 0, gpart = 0;                         // the same, a few tokens
   size_t total = 0;
@@ -50,6 +50,7 @@ DeltaLayout delta_layout(const ccq_delta_shape* s, bool bwd) {
   L.Tm = take(nchunk * 64 * 64 * e);
   if (s->io_dtype == CCQ_BF16) L.TmLo = take(nchunk * 64 * 64 * e);
   L.gam = take(nchunk * 5 * 64 * sizeof(float));
+  L.gamLo = take(nchunk * 64 * sizeof(float));
   L.U = take(nchunk * 64 * s->dv * e);
   if (bwd && ccq::delta_short(s->B, s->T, s->HV, s->io_dtype == CCQ_BF16)) {
     L.hist = take(ccq::delta_short_hist(s->B, s->T, s->HV, s->dk, s->dv) * sizeof(float));
@@ -106,6 +107,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
   const bool bf = s->io_dtype == CCQ_BF16;
   const int B = s->B, T = s->T, H = s->HV;
   float* gam = reinterpret_cast<float*>(ws + L.gam);
+  float* gamLo = reinterpret_cast<float*>(ws + L.gamLo);
   trace_begin_call();
   // a few tokens: the gradients token by token, the chunked form where o or ST is wanted
   const bool few = g && ccq::delta_short(B, T, H, bf);
@@ -124,6 +126,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
   ta.cu = cu;
   ta.HK = s->HK;
   ta.TmLo = bf ? ws + L.TmLo : nullptr;
+  ta.gamLo = gamLo;
   if (traced(st, [&] { return ccq::launch_gdn_tri(ta, bf, st); }) != hipSuccess) return CCQ_ERR_HIP;
   const int group = ccq::gdn_out_group(B, H, T, s->dk, s->dv, bf);
   ccq::GdnArgs sa{k, v, beta, ws + L.Tm, gam, S0, ST, ws + L.states, ws + L.U, B, T, H, s->dk, s->dv};
@@ -139,6 +142,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
     oa.group = group;
     oa.cu = cu;
     oa.HK = s->HK;
+    oa.gamLo = gamLo;
     if (traced(st, [&] { return ccq::launch_gdn_out(oa, bf, st); }) != hipSuccess) return CCQ_ERR_HIP;
   }
   if (!g) return CCQ_OK;
@@ -146,6 +150,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
   ccq::GdnPrepArgs pa{q, k, gam, ws + L.Tm, ws + L.PT, ws + L.TmT, B, T, H, s->dk, s->dv};
   pa.cu = cu;
   pa.HK = s->HK;
+  pa.gamLo = gamLo;
   if (traced(st, [&] { return ccq::launch_gdn_bwd_prep(pa, bf, st); }) != hipSuccess) return CCQ_ERR_HIP;
   ccq::GdnDstateArgs da{q, k, g->dO, gam, ws + L.PT, ws + L.TmT, ws + L.dstates, ws + L.dR, B, T, H, s->dk, s->dv,
                         s->scale};
@@ -180,6 +185,7 @@ ccq_status run_delta(const ccq_delta_shape* s, const int32_t* cu, bool packed, c
   ba.scale = s->scale;
   ba.cu = cu;
   ba.HK = s->HK;
+  ba.gamLo = gamLo;
   if (traced(st, [&] { return ccq::launch_gdn_bwd_chunk(ba, bf, st); }) != hipSuccess) return CCQ_ERR_HIP;
   if (s->HK != s->HV) {
     ccq::HeadSumArgs ha{ba.dqc, ba.dk_bb, g->dq, g->dk, B, T, s->HK, H, s->dk};
