@@ -621,7 +621,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       const float pm = e * dP[jj][r];
       const float ea = j < i ? -e * dA[jj][r] : 0.f;  // (M o dA)_ij
       const float E = sBeta[i] * ea;
-      const float F = pm * QK[jj][r];
+      // (a diagonal F enters dgamma_i and leaves it again: the plain rule leaves it out, so
+      // that dlogalpha under steep gates, e^-5 of it, does not carry its rounding)
+      const float F = PLAIN && j == i ? 0.f : pm * QK[jj][r];
       const float fa = ea * KK[jj][r];
       rowF[r] += F;
       rowA[r] += fa;
@@ -830,10 +832,12 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
       const float G = __expf(sGam[i]), bt = sBeta[i];
       const float colF = sColF[0][i] + sColF[1][i] + sColF[2][i] + sColF[3][i];
       const float colA = sColA[0][i] + sColA[1][i] + sColA[2][i] + sColA[3][i];
-      const float dg = G * d1[r] + rf[r] - colF - bt * G * d2[r] + bt * ra[r] - colA - sDec[i] * d3[r];
+      // (as with F, the last row's own term, which comes back through gamma_C)
+      const float t3 = PLAIN && i == nrow - 1 ? 0.f : sDec[i] * d3[r];
+      const float dg = G * d1[r] + rf[r] - colF - bt * G * d2[r] + bt * ra[r] - colA - t3;
       if (c16 == 0) {
         sDg[i] = i < nrow ? dg : 0.f;
-        xt += i < nrow ? sDec[i] * d3[r] : 0.f;
+        xt += i < nrow ? t3 : 0.f;
         if (i < nrow) {
           const size_t ti = seq_idx(sq, r0 + i, h, a.H);
           const float dbt = sRV[i] - G * d2[r] + ra[r];

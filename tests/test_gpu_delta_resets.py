@@ -45,7 +45,7 @@ def test_forward(lens, HK, HV, dk, dv, kind):
     check(got, ref, FWD_TOL)
 
 
-@pytest.mark.parametrize("kind", ["front", "half", "most"])
+@pytest.mark.parametrize("kind", ["front", "half", "most", "steep"])
 @pytest.mark.parametrize("lens,HK,HV,dv", [([130, 130], 2, 2, 64), ([64, 3, 0, 100], 1, 3, 128)])
 def test_training_step(lens, HK, HV, dv, kind):
     d = make(lens, HK, HV, 64, dv, F32, True)
