@@ -1033,8 +1033,12 @@ def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=Non
     dense = x.is_contiguous()
     ld, size = C if dense else _pitch(x, 1, "x"), x.element_size()
     x0, s0 = x.data_ptr(), state.data_ptr()
-    if x0 < s0 + B * (W - 1) * C * size and s0 < x0 + B * ld * size:
-        raise ValueError("state: shares memory with x")
+    s1 = s0 + B * (W - 1) * C * size
+    if x0 < s1 and s0 < x0 + B * ld * size:  # (no further than the last token's pitch)
+        # the first token that ends behind the state's start, and whether it is there and begins ahead of its end
+        i = max(0, (s0 - x0 - C * size) // (ld * size) + 1)
+        if i < B and x0 + i * ld * size < s1:
+            raise ValueError("state: shares memory with x")
     if out is None:
         y = torch.empty_like(x) if dense else torch.empty((B, C), dtype=dt, device=dev)
     else:
