@@ -289,7 +289,9 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * (ccq_delta_step: of the tokens behind it), never another sequence or head.
  * Supported: dv in {64,128,256,512}; dk in {64,128,256} (bf16 io) or {64,128} (fp32
  * io); the training step with fp32 io: dk = 64; ccq_delta_step: dk in {64,128,256},
- * both types.  B > 65535 packed is CCQ_ERR_UNSUPPORTED.
+ * both types.  B > 65535 packed is CCQ_ERR_UNSUPPORTED, and so are sizes that a launch
+ * cannot count: HV max(dk, dv) above 2^24; B HV ceil(T / 64) from 2^23 on, and B HV dv
+ * from 2^29 (dk = 256: 2^28) on; for ccq_delta_step B HV dv from 2^28 on.
  */
 typedef struct {
   int32_t B, T;         /* sequences, tokens (or the bound on them); >= 0 */

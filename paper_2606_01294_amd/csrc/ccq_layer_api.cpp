@@ -20,6 +20,7 @@ bool overlap(const void* p, size_t n, const void* q, size_t m) {
 }
 
 // ---- delta rule ------------------------------------------------------------
+bool delta_rows_ok(const ccq_delta_shape* s) { return (long long)s->HV * (s->dk > s->dv ? s->dk : s->dv) <= (1LL << 24); }
 ccq_status check_delta(const ccq_delta_shape* s, bool bwd) {
   if (!s) return CCQ_ERR_INVALID_ARG;
   if (s->B < 0 || s->T < 0 || s->HK < 0 || s->HV < 0 || !dtype_ok(s->io_dtype)) return CCQ_ERR_INVALID_ARG;
@@ -27,9 +28,11 @@ ccq_status check_delta(const ccq_delta_shape* s, bool bwd) {
   const bool bf = s->io_dtype == CCQ_BF16;
   if (!ccq::gdn_supported(s->dk, s->dv, bf)) return CCQ_ERR_UNSUPPORTED;
   if (bwd && !ccq::bwd_supported(s->dk, s->dv, bf, true)) return CCQ_ERR_UNSUPPORTED;
-  // 32-bit grids; 64-bit token offsets
+  // 64-bit token offsets; a launch's threads (up to 512 a chunk, 256 a tile of 16 value
+  // channels at dk = 256, 128 below) and the offsets within a chunk are 32 bits wide
   const long long bh = (long long)s->B * s->HV;
-  if (bh > (1LL << 24) || bh * ((s->T + 63LL) / 64) > (1LL << 30)) return CCQ_ERR_UNSUPPORTED;
+  if (bh * ((s->T + 63LL) / 64) >= (1LL << 23) || !delta_rows_ok(s)) return CCQ_ERR_UNSUPPORTED;
+  if (bh * s->dv >= (s->dk == 256 ? 1LL << 28 : 1LL << 29)) return CCQ_ERR_UNSUPPORTED;
   if (bh * s->T * (s->dk > s->dv ? s->dk : s->dv) > (1LL << 40)) return CCQ_ERR_UNSUPPORTED;
   return CCQ_OK;
 }
@@ -359,7 +362,8 @@ ccq_status ccq_delta_step(const ccq_delta_shape* s, const void* q, const void* k
   if (s->B < 0 || s->T < 0 || s->HK < 0 || s->HV < 0 || !dtype_ok(s->io_dtype)) return CCQ_ERR_INVALID_ARG;
   if (s->HV > 0 && (s->HK == 0 || s->HV % s->HK != 0)) return CCQ_ERR_INVALID_ARG;
   if (!ccq::decode_supported(s->dk, s->dv)) return CCQ_ERR_UNSUPPORTED;
-  if ((long long)s->B * s->HV > (1LL << 24)) return CCQ_ERR_UNSUPPORTED;
+  // 16 threads a row of the state, and a launch's threads are 32 bits wide
+  if ((long long)s->B * s->HV * s->dv >= (1LL << 28) || !delta_rows_ok(s)) return CCQ_ERR_UNSUPPORTED;
   if (s->B == 0 || s->HV == 0 || s->T == 0) return CCQ_OK;
   const void* req[] = {q, k, v, logalpha, beta, S, o};
   for (const void* p : req)
