@@ -378,7 +378,7 @@ constexpr int kSumCols = 16, kSumRows = 64;
 __global__ __launch_bounds__(kSumCols * kSumRows) void colsum_kernel(const ColsumArgs a) {
   __shared__ float buf[kSumRows][kSumCols + 1];
   const int cl = threadIdx.x % kSumCols, rl = threadIdx.x / kSumCols;
-  const int col = blockIdx.x * kSumCols + cl;
+  const int col = (int)(blockIdx.y * gridDim.x + blockIdx.x) * kSumCols + cl;
   constexpr int U = 8;
   float s[U] = {};
   if (col < a.cols) {
@@ -411,7 +411,10 @@ __global__ __launch_bounds__(kSumCols * kSumRows) void colsum_kernel(const Colsu
 }
 
 hipError_t launch_colsum(const ColsumArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(colsum_kernel, dim3((a.cols + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumRows), 0, st, a);
+  // (2^24 channels of four taps and a bias are 5 2^20 workgroups of 1024: more threads than one
+  // dimension of a launch counts)
+  const unsigned n = (unsigned)((a.cols + kSumCols - 1) / kSumCols), gx = n < (1u << 20) ? n : 1u << 20;
+  hipLaunchKernelGGL(colsum_kernel, dim3(gx, (n + gx - 1) / gx), dim3(kSumCols * kSumRows), 0, st, a);
   return hipGetLastError();
 }
 
