@@ -9,6 +9,7 @@ missing the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import threading
@@ -202,19 +203,34 @@ def _stream(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
-def _record(stream, *objs):
-    """Tensors the binding allocated on torch's current stream but handed to the
-    library on another stream `stream`: mark them as used there, so that the caching
-    allocator does not give their memory to a later allocation on the current stream
-    while the library's kernels on `stream` may still use it (the workspace is freed
-    when the call returns)."""
+# Calls on a stream that is not torch's current one (stream=s).  A call is ordered behind what s
+# has been given, and behind nothing else: s must have waited for whoever wrote the inputs, and who
+# reads the outputs elsewhere waits for s.  Memory follows that order too: what the binding
+# allocates comes from s's own pool (_pool), since a block that the current stream has freed may
+# still be written by its pending kernels, and every tensor of a call is marked as used where it is
+# (_record), so that no memory is handed on while a kernel may still use it.
+_SAME = contextlib.nullcontext()
+
+
+def _pool(stream):
+    """The context in which a call on `stream` allocates."""
+    return _SAME if stream is None else torch.cuda.stream(stream)
+
+
+def _record(stream, outs, *others):
+    """Marks a call's tensors (tensors, dicts or lists of them, or None) as used on `stream`, and the
+    outputs on the current stream as well, where the caller may drop them."""
     if stream is None:
         return
-    for o in objs:
-        for t in (o.values() if isinstance(o, dict) else (o,)):
-            if isinstance(t, torch.Tensor) and t.is_cuda and \
-                    stream != torch.cuda.current_stream(t.device):
+    here = torch.cuda.current_stream(stream.device)
+    if stream == here:
+        return
+    for i, o in enumerate((outs,) + others):
+        for t in o.values() if isinstance(o, dict) else o if isinstance(o, (list, tuple)) else (o,):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
                 t.record_stream(stream)
+                if i == 0:
+                    t.record_stream(here)
 
 
 def _check(t, name, shape, dtype, device):
@@ -259,15 +275,16 @@ def _fwd(backbone, q, k, v, gate, lam, beta, S0, C0, mu0, scale, centered, t0, c
     _check(C0, "C0", (B, H, dk, dk), torch.float32, dev)
     _check(mu0, "mu0", (B, H, dk), torch.float32, dev)
     out = dict(out or {})
-    if "o" not in out:
-        out["o"] = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
-    if want_states:
-        out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
-        out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
-        out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
-    if want_qclean:
-        out.setdefault("qclean", torch.empty((B, T, H, dk), dtype=torch.float32, device=dev))
-    workspace, need = _workspace(shape, backbone, False, workspace, dev)
+    with _pool(stream):
+        if "o" not in out:
+            out["o"] = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
+        if want_states:
+            out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
+            out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
+            out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
+        if want_qclean:
+            out.setdefault("qclean", torch.empty((B, T, H, dk), dtype=torch.float32, device=dev))
+        workspace, need = _workspace(shape, backbone, False, workspace, dev)
     st = _stream(stream)
     if backbone == CCQ_GLA:
         rc = lib().ccq_gla_fwd(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(gate), _p(lam),
@@ -281,7 +298,7 @@ def _fwd(backbone, q, k, v, gate, lam, beta, S0, C0, mu0, scale, centered, t0, c
                                _p(out.get("ST")), _p(out.get("CT")), _p(out.get("muT")),
                                _p(out.get("qclean")), _p(workspace), workspace.numel(), st)
         fn = "ccq_gdn_fwd"
-    _record(stream, workspace, out)
+    _record(stream, out, workspace, (q, k, v, gate, lam, beta, S0, C0, mu0))
     if rc != 0:
         raise CcqError(fn, rc)
     return out
@@ -329,19 +346,20 @@ def ccq_gdn_fwd_noalloc(q, k, v, logalpha, beta, lam, S0=None, C0=None, mu0=None
     _check(C0, "C0", (B, H, dk, dk), torch.float32, dev)
     _check(mu0, "mu0", (B, H, dk), torch.float32, dev)
     out = dict(out or {})
-    if "o" not in out:
-        out["o"] = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
-    if want_states:
-        out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
-        out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
-        out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
-    if want_qclean:
-        out.setdefault("qclean", torch.empty((B, T, H, dk), dtype=torch.float32, device=dev))
+    with _pool(stream):
+        if "o" not in out:
+            out["o"] = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
+        if want_states:
+            out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
+            out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
+            out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
+        if want_qclean:
+            out.setdefault("qclean", torch.empty((B, T, H, dk), dtype=torch.float32, device=dev))
     rc = lib().ccq_gdn_fwd_noalloc(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(logalpha),
                                    _p(beta), _p(lam), _p(S0), _p(C0), _p(mu0), _p(out["o"]),
                                    _p(out.get("ST")), _p(out.get("CT")), _p(out.get("muT")),
                                    _p(out.get("qclean")), _stream(stream))
-    _record(stream, out)
+    _record(stream, out, (q, k, v, logalpha, beta, lam, S0, C0, mu0))
     if rc != 0:
         raise CcqError("ccq_gdn_fwd_noalloc", rc)
     return out
@@ -373,20 +391,21 @@ def ccq_fwd_bwd(q, k, v, g, lam, dO, scale=1.0, centered=True, chunk=64, out=Non
     _check(dO, "dO", (B, T, H, dv), q.dtype, dev)
     _check(lam, "lam", (B, T, H), torch.float32, dev)
     out = dict(out or {})
-    out.setdefault("o", torch.empty((B, T, H, dv), dtype=q.dtype, device=dev))
-    out.setdefault("dq", torch.empty((B, T, H, dk), dtype=q.dtype, device=dev))
-    out.setdefault("dk", torch.empty((B, T, H, dk), dtype=q.dtype, device=dev))
-    out.setdefault("dv", torch.empty((B, T, H, dv), dtype=q.dtype, device=dev))
-    out.setdefault("dg", torch.empty(tuple(g.shape), dtype=g.dtype, device=dev))
-    out.setdefault("dlam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
-    if backbone == CCQ_GDN:
-        out.setdefault("dbeta", torch.empty((B, T, H), dtype=torch.float32, device=dev))
-    workspace, need = _workspace(shape, backbone, True, workspace, dev)
+    with _pool(stream):
+        out.setdefault("o", torch.empty((B, T, H, dv), dtype=q.dtype, device=dev))
+        out.setdefault("dq", torch.empty((B, T, H, dk), dtype=q.dtype, device=dev))
+        out.setdefault("dk", torch.empty((B, T, H, dk), dtype=q.dtype, device=dev))
+        out.setdefault("dv", torch.empty((B, T, H, dv), dtype=q.dtype, device=dev))
+        out.setdefault("dg", torch.empty(tuple(g.shape), dtype=g.dtype, device=dev))
+        out.setdefault("dlam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
+        if backbone == CCQ_GDN:
+            out.setdefault("dbeta", torch.empty((B, T, H), dtype=torch.float32, device=dev))
+        workspace, need = _workspace(shape, backbone, True, workspace, dev)
     rc = lib().ccq_fwd_bwd(ctypes.byref(shape), int(backbone), _p(q), _p(k), _p(v), _p(g),
                            _p(beta), _p(lam), _p(dO), _p(out["o"]), _p(out["dq"]),
                            _p(out["dk"]), _p(out["dv"]), _p(out["dg"]), _p(out.get("dbeta")),
                            _p(out["dlam"]), _p(workspace), workspace.numel(), _stream(stream))
-    _record(stream, workspace, out)
+    _record(stream, out, workspace, (q, k, v, g, beta, lam, dO))
     if rc != 0:
         raise CcqError("ccq_fwd_bwd", rc)
     return out
@@ -440,12 +459,13 @@ def _varlen_fwd(backbone, q, k, v, gate, beta, lam, cu_seqlens, max_len, S0, C0,
     _check(C0, "C0", (B, H, dk, dk), torch.float32, dev)
     _check(mu0, "mu0", (B, H, dk), torch.float32, dev)
     out = dict(out or {})
-    out.setdefault("o", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
-    if want_states:
-        out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
-        out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
-        out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
-    workspace = _varlen_ws(shape, backbone, False, workspace, dev)
+    with _pool(stream):
+        out.setdefault("o", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
+        if want_states:
+            out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
+            out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
+            out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
+        workspace = _varlen_ws(shape, backbone, False, workspace, dev)
     st = _stream(stream)
     if backbone == CCQ_GLA:
         rc = lib().ccq_gla_fwd_varlen(ctypes.byref(shape), _p(cu_seqlens), _p(q), _p(k), _p(v),
@@ -459,7 +479,7 @@ def _varlen_fwd(backbone, q, k, v, gate, beta, lam, cu_seqlens, max_len, S0, C0,
                                       _p(out["o"]), _p(out.get("ST")), _p(out.get("CT")),
                                       _p(out.get("muT")), _p(workspace), workspace.numel(), st)
         fn = "ccq_gdn_fwd_varlen"
-    _record(stream, workspace, out)
+    _record(stream, out, workspace, (cu_seqlens, q, k, v, gate, beta, lam, S0, C0, mu0))
     if rc != 0:
         raise CcqError(fn, rc)
     return out
@@ -527,21 +547,22 @@ def ccq_fwd_bwd_varlen(q, k, v, g, lam, dO, cu_seqlens, max_len, scale=1.0, cent
     if out:
         q, k, v, g, beta, lam, dO = _apart(stream, out, q, k, v, g, beta, lam, dO)
     out = dict(out or {})
-    out.setdefault("o", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
-    out.setdefault("dq", torch.empty((rows, H, dk), dtype=q.dtype, device=dev))
-    out.setdefault("dk", torch.empty((rows, H, dk), dtype=q.dtype, device=dev))
-    out.setdefault("dv", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
-    out.setdefault("dg", torch.empty(tuple(g.shape), dtype=g.dtype, device=dev))
-    out.setdefault("dlam", torch.empty((rows, H), dtype=torch.float32, device=dev))
-    if backbone == CCQ_GDN:
-        out.setdefault("dbeta", torch.empty((rows, H), dtype=torch.float32, device=dev))
-    workspace = _varlen_ws(shape, backbone, True, workspace, dev)
+    with _pool(stream):
+        out.setdefault("o", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
+        out.setdefault("dq", torch.empty((rows, H, dk), dtype=q.dtype, device=dev))
+        out.setdefault("dk", torch.empty((rows, H, dk), dtype=q.dtype, device=dev))
+        out.setdefault("dv", torch.empty((rows, H, dv), dtype=q.dtype, device=dev))
+        out.setdefault("dg", torch.empty(tuple(g.shape), dtype=g.dtype, device=dev))
+        out.setdefault("dlam", torch.empty((rows, H), dtype=torch.float32, device=dev))
+        if backbone == CCQ_GDN:
+            out.setdefault("dbeta", torch.empty((rows, H), dtype=torch.float32, device=dev))
+        workspace = _varlen_ws(shape, backbone, True, workspace, dev)
     rc = lib().ccq_fwd_bwd_varlen(ctypes.byref(shape), int(backbone), _p(cu_seqlens), _p(q),
                                   _p(k), _p(v), _p(g), _p(beta), _p(lam), _p(dO), _p(out["o"]),
                                   _p(out["dq"]), _p(out["dk"]), _p(out["dv"]), _p(out["dg"]),
                                   _p(out.get("dbeta")), _p(out["dlam"]), _p(workspace),
                                   workspace.numel(), _stream(stream))
-    _record(stream, workspace, out)
+    _record(stream, out, workspace, (cu_seqlens, q, k, v, g, beta, lam, dO))
     if rc != 0:
         raise CcqError("ccq_fwd_bwd_varlen", rc)
     return out
@@ -577,21 +598,27 @@ def ccq_decode(q, k, v, gate, lam, S, C, mu, t0, backbone=CCQ_GLA, beta=None, sc
             (S, "S", (B, H, dv, dk), f32), (C, "C", (B, H, dk, dk), f32), (mu, "mu", key, f32)):
         if t is None or t.shape != shp or t.dtype != d or t.device != dev or not t.is_contiguous():
             _check(t, name, shp, d, dev)
-    o = torch.empty(val, dtype=dt, device=dev) if out is None else out
-    if out is not None:
+    if out is None and stream is None:
+        o = torch.empty(val, dtype=dt, device=dev)
+    elif out is None:
+        with _pool(stream):
+            o = torch.empty(val, dtype=dt, device=dev)
+    else:
+        o = out
         _check(o, "o", val, dt, dev)
     shape = Shape(B, 1, H, dk, dv, 64, io, _dt(gate.dtype) if gla else io, float(scale),
                   1 if centered else 0, 0, int(t0))
     if workspace is None:
         need = ccq_decode_workspace_size(shape)
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            with _pool(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     rc = lib().ccq_decode(shape, int(backbone), q.data_ptr(), _p(k), v.data_ptr(), _p(gate),
                           _p(beta), _p(lam), S.data_ptr(), C.data_ptr(), mu.data_ptr(),
                           o.data_ptr(), _p(workspace),
                           0 if workspace is None else workspace.numel(), _stream(stream))
     if stream is not None:
-        _record(stream, workspace, o)
+        _record(stream, o, workspace, (q, k, v, gate, beta, lam, S, C, mu))
     if rc != 0:
         raise CcqError("ccq_decode", rc)
     return o
@@ -609,13 +636,14 @@ def ccq_prep(q_raw, k_raw, w_lam, b_lam, out=None, stream=None):
     _check(w_lam, "w_lam", (H, H * dk), torch.float32, dev)
     _check(b_lam, "b_lam", (H,), torch.float32, dev)
     out = dict(out or {})
-    out.setdefault("q", torch.empty_like(q_raw))
-    out.setdefault("k", torch.empty_like(k_raw))
-    out.setdefault("lam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
+    with _pool(stream):
+        out.setdefault("q", torch.empty_like(q_raw))
+        out.setdefault("k", torch.empty_like(k_raw))
+        out.setdefault("lam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
     shape = make_shape(B, T, H, dk, dk, q_raw.dtype)
     rc = lib().ccq_prep(ctypes.byref(shape), _p(q_raw), _p(k_raw), _p(w_lam), _p(b_lam),
                         _p(out["q"]), _p(out["k"]), _p(out["lam"]), _stream(stream))
-    _record(stream, out)
+    _record(stream, out, (q_raw, k_raw, w_lam, b_lam))
     if rc != 0:
         raise CcqError("ccq_prep", rc)
     return out
@@ -653,21 +681,22 @@ def ccq_fwd_raw(q_raw, k_raw, w_lam, b_lam, v, gate, beta=None, backbone=CCQ_GLA
     _check(C0, "C0", (B, H, dk, dk), torch.float32, dev)
     _check(mu0, "mu0", (B, H, dk), torch.float32, dev)
     out = dict(out or {})
-    out.setdefault("o", torch.empty((B, T, H, dv), dtype=q_raw.dtype, device=dev))
-    if want_states:
-        out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
-        out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
-        out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
-    if want_lam:
-        out.setdefault("lam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
-    need = ccq_fwd_raw_workspace_size(shape, backbone)
-    if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    with _pool(stream):
+        out.setdefault("o", torch.empty((B, T, H, dv), dtype=q_raw.dtype, device=dev))
+        if want_states:
+            out.setdefault("ST", torch.empty((B, H, dv, dk), dtype=torch.float32, device=dev))
+            out.setdefault("CT", torch.empty((B, H, dk, dk), dtype=torch.float32, device=dev))
+            out.setdefault("muT", torch.empty((B, H, dk), dtype=torch.float32, device=dev))
+        if want_lam:
+            out.setdefault("lam", torch.empty((B, T, H), dtype=torch.float32, device=dev))
+        need = ccq_fwd_raw_workspace_size(shape, backbone)
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
     rc = lib().ccq_fwd_raw(ctypes.byref(shape), int(backbone), _p(q_raw), _p(k_raw), _p(w_lam),
                            _p(b_lam), _p(v), _p(gate), _p(beta), _p(S0), _p(C0), _p(mu0),
                            _p(out["o"]), _p(out.get("ST")), _p(out.get("CT")), _p(out.get("muT")),
                            _p(out.get("lam")), _p(workspace), workspace.numel(), _stream(stream))
-    _record(stream, workspace, out)
+    _record(stream, out, workspace, (q_raw, k_raw, w_lam, b_lam, v, gate, beta, S0, C0, mu0))
     if rc != 0:
         raise CcqError("ccq_fwd_raw", rc)
     return out
@@ -830,14 +859,15 @@ def _delta_fwd(q, k, v, logalpha, beta, cu_seqlens, max_len, S0, scale, want_sta
     want = {"o": v}
     if want_states:
         want["ST"] = (state, torch.float32)
-    res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0))
-    ws = _scratch(workspace, ccq_delta_workspace_size(shape), dev)
+    with _pool(stream):
+        res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0))
+        ws = _scratch(workspace, ccq_delta_workspace_size(shape), dev)
     args = [q, k, v, logalpha, beta, S0, res["o"], res.get("ST")]
     if cu_seqlens is None:
         _launch("ccq_delta_fwd", dev, stream, shape, args, ws)
     else:
         _launch("ccq_delta_fwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
-    _record(stream, ws, res)
+    _record(stream, res, ws, args, cu_seqlens)
     return res
 
 
@@ -871,15 +901,16 @@ def _delta_fwd_bwd(q, k, v, logalpha, beta, dO, cu_seqlens, max_len, S0, scale, 
         want["o"] = v
     if want_states:
         want["ST"] = (state, torch.float32)
-    res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0, dO))
-    ws = _scratch(workspace, ccq_delta_workspace_size(shape, True), dev)
+    with _pool(stream):
+        res = _outputs(out, want, dev, (q, k, v, logalpha, beta, S0, dO))
+        ws = _scratch(workspace, ccq_delta_workspace_size(shape, True), dev)
     args = [q, k, v, logalpha, beta, S0, dO, res.get("o"), res.get("ST"), res["dq"], res["dk"],
             res["dv"], res["dlogalpha"], res["dbeta"]]
     if cu_seqlens is None:
         _launch("ccq_delta_fwd_bwd", dev, stream, shape, args, ws)
     else:
         _launch("ccq_delta_fwd_bwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
-    _record(stream, ws, res)
+    _record(stream, res, ws, args, cu_seqlens)
     return res
 
 
@@ -915,14 +946,15 @@ def ccq_delta_step(q, k, v, logalpha, beta, S, scale=1.0, out=None, stream=None)
                             (v, "v", (B, T, HV, dv), dt), (logalpha, "logalpha", (B, T, HV), f32),
                             (beta, "beta", (B, T, HV), f32), (S, "S", (B, HV, dv, dk), f32)):
         _check(t, name, shp, d, dev)
-    if out is None:
+    if out is None and stream is None:
         o = torch.empty_like(v)
     else:
-        o = _outputs({"o": out}, {"o": v}, dev, (q, k, v, logalpha, beta, S))["o"]
+        with _pool(stream):
+            o = _outputs({"o": out}, {"o": v}, dev, (q, k, v, logalpha, beta, S))["o"]
     shape = DeltaShape(B, T, HK, HV, dk, dv, _dt(dt), scale)
     _launch("ccq_delta_step", dev, stream, shape, (q, k, v, logalpha, beta, S, o))
     if stream is not None:
-        _record(stream, o)
+        _record(stream, o, (q, k, v, logalpha, beta, S))
     return o
 
 
@@ -952,13 +984,14 @@ def _conv_fwd(x, w, cu_seqlens, max_len, bias, state0, act, want_state, out, str
     want = {"y": x if x.is_contiguous() else (tuple(x.shape), x.dtype)}
     if want_state:
         want["stateT"] = ((shape.B, shape.W - 1, shape.C), x.dtype)
-    res = _outputs(out, want, dev, (x, w, bias, state0))
+    with _pool(stream):
+        res = _outputs(out, want, dev, (x, w, bias, state0))
     args = [x, w, bias, state0, res["y"], res.get("stateT")]
     if cu_seqlens is None:
         _launch("ccq_conv_fwd", dev, stream, shape, args)
     else:
         _launch("ccq_conv_fwd_varlen", dev, stream, shape, [cu_seqlens] + args)
-    _record(stream, res)
+    _record(stream, res, args, cu_seqlens)
     return res
 
 
@@ -990,15 +1023,16 @@ def _conv_bwd(x, w, dy, cu_seqlens, max_len, bias, state0, dstateT, act, out, wo
         want["dbias"] = bias
     if state0 is not None:
         want["dstate0"] = state0
-    res = _outputs(out, want, dev, (x, w, bias, state0, dy, dstateT))
-    ws = _scratch(workspace, int(lib().ccq_conv_workspace_size(shape)), dev)
+    with _pool(stream):
+        res = _outputs(out, want, dev, (x, w, bias, state0, dy, dstateT))
+        ws = _scratch(workspace, int(lib().ccq_conv_workspace_size(shape)), dev)
     args = [x, w, bias, state0, dy, dstateT, res["dx"], res["dw"], res.get("dbias"),
             res.get("dstate0")]
     if cu_seqlens is None:
         _launch("ccq_conv_bwd", dev, stream, shape, args, ws)
     else:
         _launch("ccq_conv_bwd_varlen", dev, stream, shape, [cu_seqlens] + args, ws)
-    _record(stream, ws, res)
+    _record(stream, res, ws, args, cu_seqlens)
     return res
 
 
@@ -1039,14 +1073,15 @@ def ccq_conv_step(x, w, state, bias=None, act=CCQ_ACT_SILU, out=None, stream=Non
         i = max(0, (s0 - x0 - C * size) // (ld * size) + 1)
         if i < B and x0 + i * ld * size < s1:
             raise ValueError("state: shares memory with x")
-    if out is None:
+    if out is None and stream is None:
         y = torch.empty_like(x) if dense else torch.empty((B, C), dtype=dt, device=dev)
     else:
-        y = _outputs({"y": out}, {"y": ((B, C), dt)}, dev, (x, w, bias, state))["y"]
+        with _pool(stream):
+            y = _outputs({"y": out}, {"y": ((B, C), dt)}, dev, (x, w, bias, state))["y"]
     shape = ConvShape(B, 1, C, W, _dt(dt), int(act), ld)
     _launch("ccq_conv_step", dev, stream, shape, (x, w, bias, state, y))
     if stream is not None:
-        _record(stream, y)
+        _record(stream, y, (x, w, bias, state))
     return y
 
 
@@ -1082,13 +1117,14 @@ def ccq_norm_fwd(x, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, act=CC
     returns z act(gate) with a gate [..., G, D], else act(z)."""
     shape = _norm_shape(x, weight, bias, gate, kind, act, eps)
     dev = x.device
-    if out is None:
+    if out is None and stream is None:
         y = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=dev)
     else:
-        y = _outputs({"y": out}, {"y": (tuple(x.shape), x.dtype)}, dev, (x, weight, bias, gate))["y"]
+        with _pool(stream):
+            y = _outputs({"y": out}, {"y": (tuple(x.shape), x.dtype)}, dev, (x, weight, bias, gate))["y"]
     _launch("ccq_norm_fwd", dev, stream, shape, (x, weight, bias, gate, y))
     if stream is not None:
-        _record(stream, y)
+        _record(stream, y, (x, weight, bias, gate))
     return y
 
 
@@ -1107,11 +1143,12 @@ def ccq_norm_bwd(x, dy, weight=None, bias=None, gate=None, kind=CCQ_NORM_RMS, ac
         want["dbias"] = bias
     if gate is not None:
         want["dgate"] = dy
-    res = _outputs(out, want, dev, (x, dy, weight, bias, gate))
     need = int(lib().ccq_norm_workspace_size(shape)) if weight is not None else 0
-    ws = _scratch(workspace, need, dev)
+    with _pool(stream):
+        res = _outputs(out, want, dev, (x, dy, weight, bias, gate))
+        ws = _scratch(workspace, need, dev)
     _launch("ccq_norm_bwd", dev, stream, shape,
             (x, weight, bias, gate, dy, res["dx"], res.get("dweight"), res.get("dbias"),
              res.get("dgate")), ws)
-    _record(stream, ws, res)
+    _record(stream, res, ws, (x, weight, bias, gate, dy))
     return res
