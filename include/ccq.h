@@ -279,7 +279,7 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * ST keeps 17 bits of every operand whatever io_dtype is (with bf16 io, the operands
  * of the state's products are taken as a bf16 head and tail: about 4e-6 from the
  * exact state), so the state may be handed from segment to segment and to
- * ccq_delta_step.  o and the gradients carry bf16 products where io_dtype is bf16
+ * ccq_delta_step.  ST may be S0; otherwise outputs may not overlap inputs.  o and the gradients carry bf16 products where io_dtype is bf16
  * (2.5e-3 to 3.5e-3); with T <= 64 and B T HV <= 128 the gradients are formed in fp32,
  * since a norm over so few numbers does not average the products' errors out.  logalpha below -104, -infinity included, is a reset (alpha = 0).
  * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
@@ -346,7 +346,9 @@ typedef enum { CCQ_ACT_NONE = 0, CCQ_ACT_SILU = 1, CCQ_ACT_SIGMOID = 2 } ccq_act
  *   can be read where it lies); w [C,W] fp32; bias [C] fp32 or NULL; y [B,T,C]
  *   io_dtype, dense.  state0 [B,W-1,C] io_dtype: the W - 1 inputs before the first
  *   token, oldest first (NULL: zeros); stateT the same after the last one (NULL: not
- *   wanted; may not overlap state0).
+ *   wanted).  y and stateT may not overlap x, state0 or each other: a token's inputs are
+ *   read by what follows it too (CCQ_ERR_INVALID_ARG; of x and y in a packed batch, whose
+ *   rows the host does not know, the caller sees to it).
  * Supported: W in {2,3,4}, C a positive multiple of 8 up to 2^24, ldx >= C with ldx elements a
  * multiple of 16 bytes.  Packed batches: x, y [rows,C], offsets and T as above.
  */

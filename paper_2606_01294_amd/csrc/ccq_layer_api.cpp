@@ -19,6 +19,14 @@ bool overlap(const void* p, size_t n, const void* q, size_t m) {
   return p && q && a < b + m && b < a + n;
 }
 
+// Whether n bytes at p meet the first `width` bytes of one of `rows` rows, `pitch` bytes apart, at x.
+bool meets_rows(const void* p, size_t n, const void* x, size_t rows, size_t pitch, size_t width) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(x);
+  if (!p || !x || n == 0 || rows == 0) return false;
+  const size_t i = a < b + width ? 0 : (a - b - width) / pitch + 1;  // the first row that ends behind p
+  return i < rows && b + i * pitch < a + n;
+}
+
 // ---- delta rule ------------------------------------------------------------
 bool delta_rows_ok(const ccq_delta_shape* s) { return (long long)s->HV * (s->dk > s->dv ? s->dk : s->dv) <= (1LL << 24); }
 ccq_status check_delta(const ccq_delta_shape* s, bool bwd) {
@@ -223,6 +231,11 @@ ccq_status conv_forward(const ccq_conv_shape* s, const int32_t* cu, bool packed,
   const size_t sb = (size_t)s->B * (s->W - 1) * s->C * esize(s->io_dtype);
   if (overlap(state0, sb, stateT, sb)) return CCQ_ERR_INVALID_ARG;
   if (!present(w) || (s->T > 0 && (!present(x) || !present(y)))) return CCQ_ERR_INVALID_ARG;
+  // runs of tokens read the inputs ahead of their first one (rows of a packed batch are not known here)
+  const size_t e = esize(s->io_dtype), rows = (size_t)s->B * s->T, yb = packed ? 0 : rows * s->C * e;
+  if (overlap(y, yb, state0, sb) || overlap(y, yb, stateT, sb)) return CCQ_ERR_INVALID_ARG;
+  if (!packed && (meets_rows(y, yb, x, rows, s->ldx * e, s->C * e) || meets_rows(stateT, sb, x, rows, s->ldx * e, s->C * e)))
+    return CCQ_ERR_INVALID_ARG;
   if (s->T == 0 && !stateT) return CCQ_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   ccq::ConvArgs a{};
