@@ -279,9 +279,12 @@ ccq_status ccq_fwd_bwd_varlen(const ccq_shape* s, ccq_backbone bb, const int32_t
  * ST keeps 17 bits of every operand whatever io_dtype is (with bf16 io, the operands
  * of the state's products are taken as a bf16 head and tail: about 4e-6 from the
  * exact state), so the state may be handed from segment to segment and to
- * ccq_delta_step.  ST may be S0; otherwise outputs may not overlap inputs.  o and the gradients carry bf16 products where io_dtype is bf16
- * (2.5e-3 to 3.5e-3); with T <= 64 and B T HV <= 128 the gradients are formed in fp32,
- * since a norm over so few numbers does not average the products' errors out.  logalpha below -104, -infinity included, is a reset (alpha = 0).
+ * ccq_delta_step.  ST may be S0; otherwise outputs may not overlap inputs.  o and the
+ * gradients carry bf16 products where io_dtype is bf16 (2.5e-3 to 3.5e-3 of their norm);
+ * with T <= 64 and B T HV <= 128 the gradients are formed in fp32, since a norm over so
+ * few numbers does not average the products' errors out.  logalpha below -104, -infinity
+ * included, is a reset (alpha = 0); the decays between tokens are good to fp32 whatever
+ * resets stand ahead of them.
  * Packed batches as for ccq_gdn_fwd_varlen: [rows, heads, d] tensors, device offsets
  * cu_seqlens of B + 1 int32, s->T a bound on the lengths; rows behind cu[B] (and
  * behind a sequence's first T) are not written.  An infinity or NaN among a token's

@@ -18,11 +18,13 @@
 // Products and sums are fp32; y and dx are rounded once.
 //
 // 16,384 tokens of 6144 channels, bf16, W = 4: forward 85 us (403 MB, 4.7 TB/s),
-// backward 132 us (604 MB, 4.6 TB/s); 8 packed sequences of up to 2048 tokens, 2048
-// channels: backward 39 us (149 MB; runs that lie behind a sequence's end leave compute
-// units idle) and 5 us for the partial rows.  Between events (42 us), runs of 16 or 64
-// tokens took 44 and 46 us there, eight channels a lane 45, eight rows at a time 51;
-// forward, runs of 16 or 64 tokens 90 and 91 us, four rows at a time 95.
+// backward 127 us (604 MB, 4.75 TB/s) and 12 for the partial rows; 8 packed sequences of up
+// to 2048 tokens, 2048 channels: backward 39 us (149 MB, 3.8 TB/s) and 5 for the partial
+// rows; the same tokens at one length 35 and 4.5, so that 4 of it is the runs behind the
+// sequences' ends (three workgroups a compute unit have work in either form, one turn).
+// Between events (42 us), runs of 16 or 64 tokens took 44 and 46 us there, eight channels
+// a lane 45, eight rows at a time 51; forward, runs of 16 or 64 tokens 90 and 91 us, four
+// rows at a time 95.
 #include "ccq_device.h"
 #include "ccq_kernels.h"
 #include "ccq_pointwise.h"

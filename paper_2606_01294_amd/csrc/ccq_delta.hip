@@ -37,11 +37,12 @@ namespace ccq {
 // chunk ahead, into two.  A loader has one chunk in flight at most, so it waits for
 // all of its loads and counts none.
 //
-// 1.3B forward (B = 4, T = 4096, H = 8, dk = dv = 256): 170 to 187 us, 5700 cycles a chunk: 1300
-// of them products, 3300 of LDS traffic (334 KB a chunk and compute unit: K rows and
-// transposed, Tm twice, the exchange), the rest the latency of the chain K S -> sum ->
-// R -> Tm R -> update.  One wave a tile takes 167 to 178 us there, features split over
-// two 165 to 172.  Tried without gain: a deeper key ring, loads without vector
+// 1.3B forward (B = 4, T = 4096, H = 8, dk = dv = 256; features over two waves): 180 to
+// 183 us (three runs of 40 launches, the least 165), 5700 cycles a chunk: 1300 of them
+// products, 3300 of LDS traffic (334 KB a chunk and compute unit: K rows and transposed,
+// Tm twice, the exchange), the rest the latency of the chain K S -> sum -> R -> Tm R ->
+// update.  One wave a tile, in turn with it: 240 to 244 us (two tiles a workgroup), 258
+// to 263 (four).  Tried without gain: a deeper key ring, loads without vector
 // arithmetic, splitting S behind the update.  (Operands of one bf16 each: 100 us.)
 template <int DK, int NPR, int NH>
 struct DeltaTile {
@@ -428,8 +429,10 @@ __global__ __launch_bounds__(64 * (NPR * NH + 4 < 8 ? 8 : NPR * NH + 4)) void de
 // would hold the barrier there: 127 against 105 us at 512 tiles of dk = 128 with all
 // three behind it, 109 with all before), and a barrier stands before Q's products.
 // dR and dV leave through LDS and two loaders: stored by the consumers themselves,
-// two bytes a lane and row, dR held them up.  Operands are bf16, D and every sum fp32 (D and dR
-// are rounded as operands and on store).
+// two bytes a lane and row, dR held them up.  Operands are bf16 (Tm^T its head alone, s e^gamma dO
+// rounded once), D and every sum fp32 (D and dR are rounded as operands and on store): the
+// gradients are 2.5e-3 to 3.5e-3 from the exact ones where storing them in bf16 alone leaves
+// 1.7e-3; tails as further operands would lengthen the chain, which is what the scan takes.
 // 1.3B training step (B = 4, T = 4096, H = 8, dk = dv = 256): 335 us in the form of
 // gdn_dstate_kernel, which stages through registers, 235 to 240 in this one.
 template <int DK, int NPR, int NH>

@@ -841,7 +841,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gdn_bwd_chunk_kernel(const GdnBwdA
         if (i < nrow) {
           const size_t ti = seq_idx(sq, r0 + i, h, a.H);
           const float dbt = sRV[i] - G * d2[r] + ra[r];
-          if constexpr (PLAIN) {
+          if constexpr (PLAIN) {  // (the io type, as dq, dk, dv: the products' error is larger than its half step)
             static_cast<T*>(a.dbeta_io)[ti] = to<T>(dbt);
           } else {
             a.dbeta[ti] = dbt;
