@@ -36,7 +36,8 @@ namespace ccq {
 // Per chunk: PT[j][i] = e^{gamma_i - gamma_j} (qc_i . k_j) for j <= i, else 0
 // (row-major, plain order), and Tm^T with rows in acc_pos order
 // (TmT[i][acc_pos(j)] = Tm[j][i]; Tm itself is stored as Tm[j][acc_pos(i)]).
-template <typename T, int DK>
+// PLAIN: the plain rule (shared query/key heads, decays from gamma and its tail).
+template <typename T, int DK, bool PLAIN>
 __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArgs a) {
   constexpr int C = kChunk;
   constexpr int P = Pad<T>::value;
@@ -44,11 +45,12 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
   __shared__ __align__(16) T sQ[C * LDQ];
   __shared__ __align__(16) T sK[C * LDQ];
   __shared__ __align__(16) T sTm[C * LDP];
-  __shared__ float sGam[C], sGamLo[C];  // gamma, and (the plain rule) what its rounding left
+  __shared__ __align__(16) float sGam[C];
+  __shared__ __align__(16) float sGamLo[PLAIN ? C : 4];  // what the rounding of gamma left
 
   const int N = (a.T + C - 1) / C;
   const int lb = xcd_logical_block(blockIdx.x, gridDim.x);
-  const ChunkOf id = a.HK && a.cu ? chunk_of(blockIdx.x, a.B, a.HK, a.H, N) : ChunkOf{lb / N, lb % N};
+  const ChunkOf id = PLAIN && a.cu ? chunk_of(blockIdx.x, a.B, a.HK, a.H, N) : ChunkOf{lb / N, lb % N};
   const int bh = id.bh, ci = id.ci;
   const int b = bh / a.H, h = bh % a.H;
   const Seq sq = seq_of(a.cu, b, a.T), sp = padded_rows(sq, b, a.T);
@@ -61,13 +63,13 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
   {
     RowTile<T, DK> rq, rk;
     RowTile<T, C> rt;
-    const KeyHead kh = key_head(a.HK, a.H, h);
-    rq.load(static_cast<const T*>(a.qc) + seq_off(a.HK ? sq : sp, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
+    const KeyHead kh = PLAIN ? key_head(a.HK, a.H, h) : KeyHead{a.H, h};
+    rq.load(static_cast<const T*>(a.qc) + seq_off(PLAIN ? sq : sp, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     rk.load(static_cast<const T*>(a.k) + seq_off(sq, r0, kh.h, kh.H, DK), (size_t)kh.H * DK, nrow);
     rt.load(static_cast<const T*>(a.Tm) + cidx * C * C, (size_t)C, C);
     if (tid < C) {
       sGam[tid] = a.gam[cidx * 5 * C + tid];
-      sGamLo[tid] = a.gamLo ? a.gamLo[cidx * C + tid] : 0.f;
+      if constexpr (PLAIN) sGamLo[tid] = a.gamLo[cidx * C + tid];
     }
     rq.store(sQ, LDQ);
     rk.store(sK, LDQ);
@@ -86,11 +88,13 @@ __global__ __launch_bounds__(kThreads) void gdn_bwd_prep_kernel(const GdnPrepArg
     f32x4 acc = zero4();
     if (t < 10) tile_mma<T, DK>(acc, sQ + 16 * I * LDQ, LDQ, sK + 16 * J * LDQ, LDQ);
     const int j = 16 * J + c16;
+    f32x4 dg = *reinterpret_cast<const f32x4*>(sGam + 16 * I + 4 * g4) - sGam[j];
+    if constexpr (PLAIN) dg += *reinterpret_cast<const f32x4*>(sGamLo + 16 * I + 4 * g4) - sGamLo[j];
     float x[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * I + 4 * g4 + r;
-      x[r] = (t < 10 && j <= i) ? acc[r] * __expf((sGam[i] - sGam[j]) + (sGamLo[i] - sGamLo[j])) : 0.f;
+      x[r] = (t < 10 && j <= i) ? acc[r] * __expf(dg[r]) : 0.f;
     }
     store4(PT + (size_t)j * C + 16 * I + 4 * g4, x[0], x[1], x[2], x[3]);
   }
@@ -883,7 +887,8 @@ template <typename T, int DK>
 hipError_t run_prep(const GdnPrepArgs& a, hipStream_t st) {
   const int nblk = a.B * a.H * ((a.T + kChunk - 1) / kChunk);
   if (nblk == 0) return hipSuccess;
-  hipLaunchKernelGGL((gdn_bwd_prep_kernel<T, DK>), dim3(nblk), dim3(kThreads), 0, st, a);
+  if (a.HK) hipLaunchKernelGGL((gdn_bwd_prep_kernel<T, DK, true>), dim3(nblk), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((gdn_bwd_prep_kernel<T, DK, false>), dim3(nblk), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 template <typename T, int DK, int NPR, int NH>
