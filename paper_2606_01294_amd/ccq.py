@@ -222,12 +222,14 @@ def _record(stream, outs, *others):
     outputs on the current stream as well, where the caller may drop them."""
     if stream is None:
         return
-    here = torch.cuda.current_stream(stream.device)
-    if stream == here:
-        return
+    here = None
     for i, o in enumerate((outs,) + others):
         for t in o.values() if isinstance(o, dict) else o if isinstance(o, (list, tuple)) else (o,):
             if isinstance(t, torch.Tensor) and t.is_cuda:
+                if here is None:
+                    here = torch.cuda.current_stream(t.device)
+                    if stream == here:
+                        return
                 t.record_stream(stream)
                 if i == 0:
                     t.record_stream(here)
